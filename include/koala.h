@@ -49,6 +49,7 @@ extern "C" {
 
 #define KOALA_FP32 0
 #define KOALA_BF16 1
+#define KOALA_FP16 2 /* tensors of the koala_kv4_* calls only */
 
 #define KOALA_EAGLE 0  /* autoregressive head: Embedding -> Linear -> K x Decoder Layer -> LM Head */
 #define KOALA_MEDUSA 1 /* non-autoregressive heads: K x ResBlock -> (shared) Linear             */
@@ -306,6 +307,89 @@ size_t koala_gemm_static_scratch_bytes(void);
 int koala_gemm_bf16_static(const void *X, const void *X_lo, const void *W, float *Y, int ldy, int M,
                            int N_out, int K_in, int split_k, void *cuda_stream,
                            int *device_status /* device int, may be NULL */);
+
+/* ---- Paged key/value cache of 4 bits ---------------------------------------------------------------------------
+ *
+ * Keys and values of n_layers layers in pages of page_size slots; a page holds all kv heads of one layer, and page i of
+ * every layer belongs together, so that one page table serves all layers.  A vector x of head_dim numbers (the rotated key or
+ * the value of one token and kv head) is held as codes 0..15 and two bf16 numbers,
+ *     zero = the largest bf16 not above min x,  scale = the smallest bf16 not below fl((max x - zero) / 15),
+ *     code = clamp(rint(fl((x - zero) / scale)), 0, 15)     (fl: rounded to fp32; ties to even)
+ * and stands for zero + scale * code, at most scale / 2 (and the rounding of fl) from x: 4.25 bits a number with heads of
+ * 128, 4.5 with 64.  A scale below 2^-100 is 0; a vector with an infinity or a NaN, or with a range that overflows, is held
+ * as NaN.  The order of the bytes inside a page is the library's own: pages are written by koala_kv4_append and
+ * koala_kv4_move and read by koala_kv4_attention and koala_kv4_read (whole pages may be copied).  Pages need no initial values.
+ *
+ * The calls are stand-alone: they need no koala_ctx, allocate nothing, enqueue kernels on `cuda_stream` of the current device
+ * and return a KOALA_* code.  What the host can see is checked before anything is enqueued.  What only the device sees (a row
+ * whose slot or position is out of range, or for which the table has no page; an impossible row_start) sets *status, if
+ * given, to KOALA_E_INVALID, and that row or sequence is left out.  Calls that may overlap on the GPU may read the same pages; a call that
+ * writes slots must be ordered against the calls that read or write the same slots.  A page that two sequences share is
+ * written by whoever appends to it: give the writer a page of its own first. */
+typedef struct {
+  uint32_t struct_size; /* sizeof(koala_kv4) */
+  int32_t n_layers, n_kv_heads;
+  int32_t head_dim;  /* 64 or 128 */
+  int32_t page_size; /* slots per page: 16, 32, 64, .. 1024 */
+  int32_t n_pages;
+  void *pages;       /* device, 128-byte aligned, koala_kv4_bytes() bytes: [n_layers][n_pages][page] */
+} koala_kv4;
+
+/* The rows of one forward: `total` tokens of B sequences, the rows of a sequence next to one another.  All pointers are
+ * DEVICE arrays; made once, it serves every layer of the forward. */
+typedef struct {
+  uint32_t struct_size;      /* sizeof(koala_kv4_rows) */
+  int32_t B;
+  int32_t total;             /* rows of the call's tensors */
+  int32_t max_rows;          /* host-known bound on the rows of one sequence; <= 128 with `slot` or `mask` */
+  int32_t table_stride;
+  const int32_t *page_table; /* [B][table_stride]: page of slots page_size * i .. ; anything outside 0 .. n_pages-1: none */
+  const int32_t *ctx_len;    /* [B] slots held before these rows: row i of a sequence lies at slot ctx_len + i */
+  const int32_t *row_start;  /* [B+1] rows row_start[b] .. row_start[b+1]-1 belong to sequence b; NULL: max_rows rows each.
+                                Rows behind the last sequence are left as they are */
+  const int32_t *kv_len;     /* [B] slots in use (attention); NULL: ctx_len + the sequence's rows */
+  const int32_t *slot;       /* [total] slots of the rows, negative: row not in use; NULL: ctx_len + i.  Of rows of a sequence
+                                with the same slot the last one is kept */
+  const uint64_t *mask;      /* [total][2] (attention): bit j: the row sees slot ctx_len + j.  NULL: it sees the slots up to ctx_len + i */
+  int32_t *status;           /* device int, or NULL */
+} koala_kv4_rows;
+
+/* [rows][heads][head_dim], strides in elements; head_dim is contiguous; addresses and strides are multiples of 4 elements. */
+typedef struct {
+  void *data;
+  int64_t row_stride, head_stride;
+} koala_kv4_tensor;
+
+/* Bytes of `pages` (0: the description is invalid). */
+size_t koala_kv4_bytes(const koala_kv4 *cache);
+
+/* Appends keys and values of the rows to one layer, the keys rotated on the way; queries are rotated to q_out (which may be q).
+ * t: HOST array of four tensors of `dtype`: k, v [total][n_kv_heads], q, q_out [total][n_heads] (q.data NULL: no queries).
+ * rope: DEVICE [n_pos][head_dim/2] pairs (cos, sin) fp32; element i is turned with element i + head_dim/2; NULL: nothing is rotated.
+ * pos: DEVICE [total] row of `rope` of each row, NULL: its slot.  Rotation in fp32, every product rounded. */
+int koala_kv4_append(const koala_kv4 *cache, int32_t layer, const koala_kv4_rows *rows, int32_t dtype,
+                     const koala_kv4_tensor *t, int32_t n_heads, const float *rope, int32_t n_pos, const int32_t *pos,
+                     void *cuda_stream);
+
+/* out = softmax(scale * q K^T) V over the slots that each row sees: those below ctx_len, and behind them by `mask` or order, below
+ * kv_len.  A row that sees nothing, or is not in use, gives 0.  Heads h of q share kv head h / (n_heads / n_kv_heads).  t: HOST array
+ * of two tensors of `dtype` [total][n_heads]: q and out (which may be q).  scratch: device, 16-byte aligned, >=
+ * koala_kv4_attention_scratch_bytes() (which may be 0), not shared by calls that may overlap.  Accumulation and softmax in fp32. */
+size_t koala_kv4_attention_scratch_bytes(const koala_kv4 *cache, const koala_kv4_rows *rows, int32_t n_heads);
+int koala_kv4_attention(const koala_kv4 *cache, int32_t layer, const koala_kv4_rows *rows, int32_t dtype,
+                        const koala_kv4_tensor *t, int32_t n_heads, float scale, void *scratch, size_t scratch_bytes,
+                        void *cuda_stream);
+
+/* The values that the rows' slots stand for.  layer < 0: all layers, layer_stride[0] (k) and [1] (v) elements apart.  t: HOST
+ * array of two tensors of `dtype` [total][n_kv_heads]: k and v (data NULL: not wanted). */
+int koala_kv4_read(const koala_kv4 *cache, int32_t layer, const koala_kv4_rows *rows, int32_t dtype, const koala_kv4_tensor *t,
+                   const int64_t *layer_stride, void *cuda_stream);
+
+/* In all layers: slot dst[b][i] of sequence b becomes what slot src[b][i] held before the call (an accepted path moves behind its
+ * context), i < n <= 128.  Entries with a negative slot are left out; of several with the same destination the last one is kept.
+ * src, dst, page_table: DEVICE [B][n], [B][n], [B][table_stride]. */
+int koala_kv4_move(const koala_kv4 *cache, int32_t B, const int32_t *page_table, int32_t table_stride, int32_t n,
+                   const int32_t *src, const int32_t *dst, int32_t *status, void *cuda_stream);
 
 #ifdef __cplusplus
 }

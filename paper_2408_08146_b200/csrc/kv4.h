@@ -1,0 +1,34 @@
+// Launchers of the paged 4-bit cache (kv4.cu, kv4_attn.cu); every one is asynchronous on its stream.
+#pragma once
+#include "kv4.cuh"
+
+namespace koala {
+
+constexpr int KV4_MAX_MOVES = 128;              // of one sequence in one call
+struct Kv4Moves {
+  int n;                                        // moves per sequence, at most KV4_MAX_MOVES
+  int stride;
+  const int32_t *src, *dst;                     // [B][stride]; entries with a negative one are left out; dst null: 0, 1, ..
+  const int32_t *base, *count;                  // [B] added to both; how many of the n are used (null: 0; n)
+  int *status;
+};
+
+// qkv: q, k, v; q rotated to q_out where n_q > 0.  rope: [n_pos][dh/2] (cos, sin) or null; pos: row of it (null: the slot).
+cudaError_t kv4_append(Launch L, int dh, int dtype, const Kv4Cache &c, size_t layer_off, const Kv4Rows &rows, const Kv4Tensor *qkv, int n_q, Kv4Tensor q_out,
+                       const float *rope, const int32_t *pos, int n_pos);
+cudaError_t kv4_read(Launch L, int dh, int dtype, const Kv4Cache &c, int layer0, int layers, const Kv4Rows &rows, Kv4Tensor k, Kv4Tensor v, long long k_layer,
+                     long long v_layer);
+cudaError_t kv4_move(Launch L, int dh, const Kv4Cache &c, int B, const Kv4Moves &m);
+
+struct Kv4Attn {
+  Kv4Cache c;
+  size_t layer_off;
+  Kv4Rows rows;
+  Kv4Tensor q, out;
+  void *out_lo;                                 // KV4_PAIR: the residuals, laid out as `out`
+  int q_type, out_type, n_heads;
+  float scale;
+};
+cudaError_t kv4_attention(Launch L, int dh, const Kv4Attn &a, int num_sms);
+
+}  // namespace koala

@@ -1,0 +1,122 @@
+// C entry points of the paged 4-bit cache: argument checks and launches.
+#include "../../include/koala.h"
+#include "kv4.h"
+
+using namespace koala;
+
+namespace {
+
+bool cache_ok(const koala_kv4 *k) {
+  if (!k || k->struct_size != sizeof(koala_kv4)) return false;
+  if (k->n_layers < 1 || k->n_kv_heads < 1 || k->n_kv_heads > 4096 || k->n_pages < 1 || (k->head_dim != 64 && k->head_dim != 128)) return false;
+  return k->page_size >= 16 && k->page_size <= 1024 && (k->page_size & (k->page_size - 1)) == 0;
+}
+bool pages_ok(const koala_kv4 *k) { return k->pages != nullptr && ((uintptr_t)k->pages & 127u) == 0; }
+
+int log2i(int v) { return 31 - __builtin_clz((unsigned)v); }
+
+size_t layer_bytes(const koala_kv4 *k) {
+  return (size_t)k->n_pages * (size_t)k->n_kv_heads * (size_t)(k->page_size / KV4_G) * (size_t)kv4_granule_bytes(k->head_dim);
+}
+
+Kv4Cache cache_of(const koala_kv4 *k, const int32_t *table, int table_stride) {
+  return Kv4Cache{(unsigned char *)k->pages, layer_bytes(k), k->n_layers, k->n_kv_heads, k->n_pages, log2i(k->page_size / KV4_G), table, table_stride};
+}
+
+// KOALA_OK, or what is wrong with the rows; whether there is anything to do is the caller's to ask (total == 0).
+int rows_ok(const koala_kv4 *k, const koala_kv4_rows *r) {
+  if (!r || r->struct_size != sizeof(koala_kv4_rows)) return KOALA_E_INVALID;
+  if (r->B < 1 || (long long)r->B * k->n_kv_heads > 65535 || r->total < 0 || r->max_rows < 1 || r->table_stride < 1) return KOALA_E_INVALID;
+  if ((long long)r->table_stride * k->page_size > (1ll << 30)) return KOALA_E_INVALID;
+  if (!r->page_table || !r->ctx_len) return KOALA_E_INVALID;
+  if (!r->row_start && (long long)r->B * r->max_rows != r->total) return KOALA_E_INVALID;
+  if ((r->slot || r->mask) && r->max_rows > KOALA_MAX_TREE) return KOALA_E_UNSUPPORTED;
+  if (r->mask && ((uintptr_t)r->mask & 7u) != 0) return KOALA_E_INVALID;
+  return KOALA_OK;
+}
+
+Kv4Rows rows_of(const koala_kv4_rows *r) {
+  return Kv4Rows{r->B, r->total, r->max_rows, r->row_start, r->ctx_len, r->kv_len, r->slot, r->mask, nullptr, r->status};
+}
+
+bool type_ok(int dtype) { return dtype == KOALA_FP32 || dtype == KOALA_BF16 || dtype == KOALA_FP16; }
+
+bool tensor_ok(const koala_kv4_tensor &t, int dtype) {
+  const uintptr_t size = dtype == KOALA_FP32 ? 4 : 2;
+  return t.data != nullptr && ((uintptr_t)t.data & (4 * size - 1)) == 0 && t.row_stride % 4 == 0 && t.head_stride % 4 == 0;
+}
+Kv4Tensor tensor_of(const koala_kv4_tensor &t) { return Kv4Tensor{t.data, t.row_stride, t.head_stride}; }
+
+int done(cudaError_t e) { return e == cudaSuccess ? KOALA_OK : KOALA_E_CUDA; }
+
+}  // namespace
+
+static_assert(KOALA_FP32 == KV4_FP32 && KOALA_BF16 == KV4_BF16 && KOALA_FP16 == KV4_FP16, "storage types");
+static_assert(KOALA_MAX_TREE == KV4_MAX_MOVES, "a tree's nodes in one call");
+
+extern "C" {
+#pragma GCC visibility push(default)
+
+size_t koala_kv4_bytes(const koala_kv4 *k) { return cache_ok(k) ? (size_t)k->n_layers * layer_bytes(k) : 0; }
+
+int koala_kv4_append(const koala_kv4 *k, int32_t layer, const koala_kv4_rows *r, int32_t dtype, const koala_kv4_tensor *t, int32_t n_heads,
+                     const float *rope, int32_t n_pos, const int32_t *pos, void *cuda_stream) {
+  if (!cache_ok(k) || !pages_ok(k) || layer < 0 || layer >= k->n_layers || !type_ok(dtype) || !t) return KOALA_E_INVALID;
+  const int rc = rows_ok(k, r);
+  if (rc != KOALA_OK) return rc;
+  const bool queries = t[2].data != nullptr;
+  if (!tensor_ok(t[0], dtype) || !tensor_ok(t[1], dtype)) return KOALA_E_INVALID;
+  if (queries && (!tensor_ok(t[2], dtype) || !tensor_ok(t[3], dtype) || n_heads < 1 || n_heads > 65536)) return KOALA_E_INVALID;
+  if (rope && (n_pos < 1 || ((uintptr_t)rope & 15u) != 0)) return KOALA_E_INVALID;
+  if (r->total == 0) return KOALA_OK;
+  const Kv4Tensor x[3] = {queries ? tensor_of(t[2]) : Kv4Tensor{nullptr, 0, 0}, tensor_of(t[0]), tensor_of(t[1])};
+  return done(kv4_append(Launch{(cudaStream_t)cuda_stream, true}, k->head_dim, dtype, cache_of(k, r->page_table, r->table_stride),
+                         (size_t)layer * layer_bytes(k), rows_of(r), x, queries ? n_heads : 0, queries ? tensor_of(t[3]) : Kv4Tensor{nullptr, 0, 0}, rope,
+                         pos, n_pos));
+}
+
+size_t koala_kv4_attention_scratch_bytes(const koala_kv4 *k, const koala_kv4_rows *r, int32_t n_heads) {
+  (void)k; (void)r; (void)n_heads;
+  return 0;
+}
+
+int koala_kv4_attention(const koala_kv4 *k, int32_t layer, const koala_kv4_rows *r, int32_t dtype, const koala_kv4_tensor *t, int32_t n_heads, float scale,
+                        void *scratch, size_t scratch_bytes, void *cuda_stream) {
+  if (!cache_ok(k) || !pages_ok(k) || layer < 0 || layer >= k->n_layers || !type_ok(dtype) || !t) return KOALA_E_INVALID;
+  const int rc = rows_ok(k, r);
+  if (rc != KOALA_OK) return rc;
+  if (!tensor_ok(t[0], dtype) || !tensor_ok(t[1], dtype)) return KOALA_E_INVALID;
+  if (n_heads < 1 || n_heads > 65536 || n_heads % k->n_kv_heads != 0 || !(scale > 0.f && scale < 1e30f)) return KOALA_E_INVALID;
+  (void)scratch; (void)scratch_bytes;
+  if (r->total == 0) return KOALA_OK;
+  const Kv4Attn a{cache_of(k, r->page_table, r->table_stride), (size_t)layer * layer_bytes(k), rows_of(r), tensor_of(t[0]), tensor_of(t[1]), nullptr,
+                  dtype, dtype, n_heads, scale};
+  return done(kv4_attention(Launch{(cudaStream_t)cuda_stream, true}, k->head_dim, a, 148));
+}
+
+int koala_kv4_read(const koala_kv4 *k, int32_t layer, const koala_kv4_rows *r, int32_t dtype, const koala_kv4_tensor *t, const int64_t *layer_stride,
+                   void *cuda_stream) {
+  if (!cache_ok(k) || !pages_ok(k) || layer >= k->n_layers || !type_ok(dtype) || !t) return KOALA_E_INVALID;
+  const int rc = rows_ok(k, r);
+  if (rc != KOALA_OK) return rc;
+  for (int i = 0; i < 2; ++i)
+    if (t[i].data && (!tensor_ok(t[i], dtype) || (layer < 0 && (!layer_stride || layer_stride[i] % 4 != 0)))) return KOALA_E_INVALID;
+  const int layers = layer < 0 ? k->n_layers : 1;
+  if (layers > 65535) return KOALA_E_UNSUPPORTED;
+  if (r->total == 0 || (!t[0].data && !t[1].data)) return KOALA_OK;
+  return done(kv4_read(Launch{(cudaStream_t)cuda_stream, true}, k->head_dim, dtype, cache_of(k, r->page_table, r->table_stride), layer < 0 ? 0 : layer, layers,
+                       rows_of(r), tensor_of(t[0]), tensor_of(t[1]), layer < 0 ? layer_stride[0] : 0, layer < 0 ? layer_stride[1] : 0));
+}
+
+int koala_kv4_move(const koala_kv4 *k, int32_t B, const int32_t *page_table, int32_t table_stride, int32_t n, const int32_t *src, const int32_t *dst,
+                   int32_t *status, void *cuda_stream) {
+  if (!cache_ok(k) || !pages_ok(k) || B < 1 || B > 65535 || !page_table || table_stride < 1 || n < 0 || !src || !dst) return KOALA_E_INVALID;
+  if ((long long)table_stride * k->page_size > (1ll << 30)) return KOALA_E_INVALID;
+  if (n > KV4_MAX_MOVES || k->n_layers > 65535) return KOALA_E_UNSUPPORTED;
+  if (n == 0) return KOALA_OK;
+  const Kv4Moves m{n, n, src, dst, nullptr, nullptr, status};
+  return done(kv4_move(Launch{(cudaStream_t)cuda_stream, true}, k->head_dim, cache_of(k, page_table, table_stride), B, m));
+}
+
+#pragma GCC visibility pop
+}  // extern "C"

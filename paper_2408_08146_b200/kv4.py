@@ -1,0 +1,243 @@
+"""The paged 4-bit key/value cache (koala_kv4_* of the C ABI): argument checks and marshalling only."""
+from __future__ import annotations
+
+import ctypes as C
+import math
+import struct
+from typing import Optional, Tuple
+
+import torch
+
+from .binding import KOALA_OK, KoalaError, load_library
+
+_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+MAX_TREE = 128
+
+
+class koala_kv4(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("n_layers", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("page_size", C.c_int32), ("n_pages", C.c_int32), ("pages", C.c_void_p)]
+
+
+class koala_kv4_rows(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("B", C.c_int32), ("total", C.c_int32), ("max_rows", C.c_int32),
+                ("table_stride", C.c_int32), ("page_table", C.c_void_p), ("ctx_len", C.c_void_p), ("row_start", C.c_void_p),
+                ("kv_len", C.c_void_p), ("slot", C.c_void_p), ("mask", C.c_void_p), ("status", C.c_void_p)]
+
+
+_lib = None
+
+
+def _library() -> C.CDLL:
+    global _lib
+    if _lib is None:
+        lib = load_library()
+        p, i = C.c_void_p, C.c_int32
+        lib.koala_kv4_bytes.restype = C.c_size_t
+        lib.koala_kv4_bytes.argtypes = [p]
+        lib.koala_kv4_append.restype = C.c_int
+        lib.koala_kv4_append.argtypes = [p, i, p, i, C.c_char_p, i, p, i, p, p]
+        lib.koala_kv4_attention_scratch_bytes.restype = C.c_size_t
+        lib.koala_kv4_attention_scratch_bytes.argtypes = [p, p, i]
+        lib.koala_kv4_attention.restype = C.c_int
+        lib.koala_kv4_attention.argtypes = [p, i, p, i, C.c_char_p, i, C.c_float, p, C.c_size_t, p]
+        lib.koala_kv4_read.restype = C.c_int
+        lib.koala_kv4_read.argtypes = [p, i, p, i, C.c_char_p, C.c_char_p, p]
+        lib.koala_kv4_move.restype = C.c_int
+        lib.koala_kv4_move.argtypes = [p, i, p, i, i, p, p, p, p]
+        _lib = lib
+    return _lib
+
+
+def rope_table(n_pos: int, head_dim: int, base: float = 10000.0, device="cuda:0") -> torch.Tensor:
+    """[n_pos][head_dim/2][cos, sin] fp32, the angles in 64 bits: position p turns pair i by p * base ** (-2 i / head_dim)."""
+    i = torch.arange(head_dim // 2, dtype=torch.float64, device=device)
+    angle = torch.arange(n_pos, dtype=torch.float64, device=device)[:, None] * base ** (-2.0 * i / head_dim)
+    return torch.stack([angle.cos(), angle.sin()], dim=-1).float().contiguous()
+
+
+class KV4Rows:
+    """The rows of one forward (koala_kv4_rows): made once, used by every layer.  Keeps its tensors alive."""
+
+    def __init__(self, c: koala_kv4_rows, total: int, device: torch.device, keep: tuple):
+        self._c, self.total, self.device, self._keep = c, total, device, keep
+        self._p = C.addressof(c)
+
+
+def _strides(t: torch.Tensor, rows: int, heads: int, dim: int, dtype: torch.dtype, device: torch.device, name: str) -> Tuple[int, int, int]:
+    if t.dtype is not dtype or t.device != device:
+        raise ValueError(f"{name} must be a {dtype} tensor on {device}")
+    if t.dim() != 3 or t.size(0) != rows or t.size(1) != heads or t.size(2) != dim:
+        raise ValueError(f"{name} must have the shape {(rows, heads, dim)}, not {tuple(t.shape)}")
+    a, b, c = t.stride()
+    if c != 1 or a % 4 or b % 4 or t.data_ptr() % (4 * t.element_size()):
+        raise ValueError(f"{name}: the last dimension must be contiguous, addresses and strides multiples of 4 elements")
+    return t.data_ptr(), a, b
+
+
+class PagedKV4:
+    """A cache of n_layers layers: n_pages pages of page_size slots for all kv heads, 4 bits a number (see include/koala.h).
+
+    Every call runs on the current stream of the cache's device and waits for nothing."""
+
+    def __init__(self, n_layers: int, n_kv_heads: int, head_dim: int, page_size: int, n_pages: int, device="cuda:0",
+                 pages: Optional[torch.Tensor] = None):
+        """pages: memory for the cache (uint8, 128-byte aligned) instead of memory of its own; page contents need no initial values."""
+        lib = _library()
+        dev = torch.device(device)
+        if dev.type == "cuda" and dev.index is None:
+            dev = torch.device("cuda", torch.cuda.current_device())
+        self.device, self.n_layers, self.n_kv_heads, self.head_dim, self.page_size, self.n_pages = dev, n_layers, n_kv_heads, head_dim, page_size, n_pages
+        c = koala_kv4(C.sizeof(koala_kv4), n_layers, n_kv_heads, head_dim, page_size, n_pages, None)
+        n = int(lib.koala_kv4_bytes(C.byref(c)))
+        if n == 0:
+            raise KoalaError(1, f"no such cache: {n_layers} layers, {n_kv_heads} heads of {head_dim}, {n_pages} pages of {page_size}")
+        if pages is None:
+            pages = torch.empty(n, dtype=torch.uint8, device=dev)
+        if pages.dtype is not torch.uint8 or pages.device != dev or not pages.is_contiguous() or pages.numel() < n or pages.data_ptr() % 128:
+            raise ValueError(f"pages must be {n} contiguous, 128-byte aligned uint8 on {dev}")
+        self.pages = pages
+        c.pages = pages.data_ptr()
+        self._c, self._p = c, C.addressof(c)
+
+    # ------------------------------------------------------------------ plans
+    def _ints(self, t: Optional[torch.Tensor], shape: Tuple[int, ...], name: str, dtype=torch.int32):
+        if t is None:
+            return None
+        if t.dtype is not dtype or t.device != self.device or tuple(t.shape) != shape or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous {dtype} tensor {shape} on {self.device}")
+        return t.data_ptr()
+
+    def _table(self, page_table: torch.Tensor) -> Tuple[int, int]:
+        if page_table.dim() != 2 or page_table.size(0) < 1 or page_table.size(1) < 1:
+            raise ValueError("page_table must be [sequences][pages of one]")
+        return self._ints(page_table, tuple(page_table.shape), "page_table"), page_table.size(1)
+
+    def rows(self, page_table: torch.Tensor, ctx_len: torch.Tensor, row_start: Optional[torch.Tensor] = None, total: Optional[int] = None,
+             max_rows: int = 1, kv_len: Optional[torch.Tensor] = None, slot: Optional[torch.Tensor] = None, mask: Optional[torch.Tensor] = None,
+             status: Optional[torch.Tensor] = None) -> KV4Rows:
+        """The rows of a forward.  page_table [B][n] and ctx_len [B] int32; row i of sequence b lies at slot ctx_len[b] + i, unless
+        `slot` [total] says otherwise (negative: not in use).  row_start [B + 1]: first row of each sequence, with `total` rows in all;
+        without it every sequence has max_rows rows.  mask [total][2] int64: bit j: the row sees slot ctx_len + j (a tree); without it a
+        row sees the slots up to ctx_len + i.  kv_len [B]: slots in use, if not ctx_len + rows.  status: int32 [1], set to
+        KOALA_E_INVALID where the device finds a row out of range."""
+        at, stride = self._table(page_table)
+        B = page_table.size(0)
+        if row_start is None:
+            total = B * max_rows if total is None else total
+        elif total is None:
+            raise ValueError("row_start needs the total number of rows")
+        if max_rows < 1 or total < 0 or (row_start is None and total != B * max_rows):
+            raise ValueError("max_rows must be positive, and total B * max_rows without row_start")
+        if (slot is not None or mask is not None) and max_rows > MAX_TREE:
+            raise ValueError(f"rows with slots or masks of their own: at most {MAX_TREE} a sequence")
+        c = koala_kv4_rows(C.sizeof(koala_kv4_rows), B, total, max_rows, stride, at, self._ints(ctx_len, (B,), "ctx_len"),
+                           self._ints(row_start, (B + 1,), "row_start"), self._ints(kv_len, (B,), "kv_len"), self._ints(slot, (total,), "slot"),
+                           self._ints(mask, (total, 2), "mask", torch.int64), self._ints(status, (1,), "status"))
+        return KV4Rows(c, total, self.device, (page_table, ctx_len, row_start, kv_len, slot, mask, status))
+
+    # ------------------------------------------------------------------ the four calls
+    def _call(self, name: str, fn, *args):
+        dev = self.device
+        if torch.cuda.current_device() != dev.index:
+            with torch.cuda.device(dev):
+                rc = fn(self._p, *args, torch.cuda.current_stream(dev).cuda_stream)
+        else:
+            rc = fn(self._p, *args, torch.cuda.current_stream(dev).cuda_stream)
+        if rc != KOALA_OK:
+            raise KoalaError(rc, name)
+
+    def _mine(self, rows: KV4Rows):
+        if rows.device != self.device:
+            raise ValueError(f"the rows are on {rows.device}, the cache on {self.device}")
+
+    def append(self, layer: int, rows: KV4Rows, k: torch.Tensor, v: torch.Tensor, rope: Optional[torch.Tensor] = None,
+               pos: Optional[torch.Tensor] = None, q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+        """Keys (rotated) and values of the rows into the cache; returns the rotated queries, in q_out if given, where there are queries.
+        k, v: [total][n_kv_heads][head_dim]; q, q_out: [total][heads][head_dim], all of one type (fp32, bf16, fp16).  rope:
+        [positions][head_dim / 2][2] fp32 (rope_table); pos: int32 [total] positions, by default the slots."""
+        self._mine(rows)
+        n, dt, dim, dev = rows.total, k.dtype, self.head_dim, self.device
+        if dt not in _TYPES:
+            raise ValueError(f"keys of type {dt}")
+        a = _strides(k, n, self.n_kv_heads, dim, dt, dev, "k") + _strides(v, n, self.n_kv_heads, dim, dt, dev, "v")
+        heads = 0
+        if q is not None:
+            heads = q.size(1)
+            if q_out is None:
+                q_out = torch.empty(q.shape, dtype=dt, device=dev)
+            a += _strides(q, n, heads, dim, dt, dev, "q") + _strides(q_out, n, heads, dim, dt, dev, "q_out")
+        else:
+            a += (0, 0, 0, 0, 0, 0)
+        table, n_pos = None, 0
+        if rope is not None:
+            if rope.dtype is not torch.float32 or rope.device != dev or rope.dim() != 3 or rope.size(1) != dim // 2 or rope.size(2) != 2 or not rope.is_contiguous():
+                raise ValueError(f"rope must be a contiguous fp32 tensor [positions][{dim // 2}][2] on {dev}")
+            table, n_pos = rope.data_ptr(), rope.size(0)
+        self._call("koala_kv4_append", _library().koala_kv4_append, layer, rows._p, _TYPES[dt], struct.pack("12q", *a), heads, table, n_pos,
+                   self._ints(pos, (n,), "pos"))
+        return q_out if q is not None else None
+
+    def attention(self, layer: int, rows: KV4Rows, q: torch.Tensor, out: Optional[torch.Tensor] = None, scale: Optional[float] = None,
+                  scratch: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """softmax(scale * q K^T) V of the rows, [total][heads][head_dim] as q (fp32, bf16, fp16); scale: 1 / sqrt(head_dim) by default.
+        scratch: uint8 of scratch_bytes(rows, heads), by default from torch's allocator."""
+        self._mine(rows)
+        dt, dim, dev, heads = q.dtype, self.head_dim, self.device, q.size(1)
+        if dt not in _TYPES:
+            raise ValueError(f"queries of type {dt}")
+        if out is None:
+            out = torch.empty(q.shape, dtype=dt, device=dev)
+        t = struct.pack("6q", *_strides(q, rows.total, heads, dim, dt, dev, "q"), *_strides(out, rows.total, heads, dim, dt, dev, "out"))
+        lib = _library()
+        need = lib.koala_kv4_attention_scratch_bytes(self._p, rows._p, heads)
+        at = None
+        if need:
+            if scratch is None:
+                scratch = torch.empty(need, dtype=torch.uint8, device=dev)
+            elif scratch.dtype is not torch.uint8 or scratch.device != dev or scratch.numel() < need or not scratch.is_contiguous():
+                raise ValueError(f"scratch must be {need} contiguous bytes on {dev}")
+            at = scratch.data_ptr()
+        self._call("koala_kv4_attention", lib.koala_kv4_attention, layer, rows._p, _TYPES[dt], t, heads,
+                   1.0 / math.sqrt(dim) if scale is None else scale, at, need)
+        return out
+
+    def scratch_bytes(self, rows: KV4Rows, heads: int) -> int:
+        return int(_library().koala_kv4_attention_scratch_bytes(self._p, rows._p, heads))
+
+    def read(self, rows: KV4Rows, layer: Optional[int] = None, dtype: torch.dtype = torch.bfloat16, k_out: Optional[torch.Tensor] = None,
+             v_out: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+        """The values that the rows' slots stand for: (k, v) [total][n_kv_heads][head_dim], with the layers in front if layer is None."""
+        self._mine(rows)
+        n, dim, dev = rows.total, self.head_dim, self.device
+        dt = dtype if k_out is None else k_out.dtype
+        if dt not in _TYPES:
+            raise ValueError(f"values of type {dt}")
+        shape = (n, self.n_kv_heads, dim) if layer is not None else (self.n_layers, n, self.n_kv_heads, dim)
+        a, layers = (), ()
+        outs = []
+        for name, t in (("k_out", k_out), ("v_out", v_out)):
+            if t is None:
+                t = torch.empty(shape, dtype=dt, device=dev)
+            if layer is None:
+                if t.dim() != 4 or t.size(0) != self.n_layers or t.stride(0) % 4:
+                    raise ValueError(f"{name} must have the shape {shape}, its layers a multiple of 4 elements apart")
+                layers += (t.stride(0),)
+                a += _strides(t[0], n, self.n_kv_heads, dim, dt, dev, name)
+            else:
+                layers += (0,)
+                a += _strides(t, n, self.n_kv_heads, dim, dt, dev, name)
+            outs.append(t)
+        self._call("koala_kv4_read", _library().koala_kv4_read, -1 if layer is None else layer, rows._p, _TYPES[dt], struct.pack("6q", *a),
+                   struct.pack("2q", *layers))
+        return outs[0], outs[1]
+
+    def move(self, page_table: torch.Tensor, src: torch.Tensor, dst: torch.Tensor, status: Optional[torch.Tensor] = None) -> None:
+        """In every layer slot dst[b][i] of sequence b becomes what slot src[b][i] held before; negative slots are left out."""
+        at, stride = self._table(page_table)
+        B = page_table.size(0)
+        if src.dim() != 2 or src.size(1) > MAX_TREE:
+            raise ValueError(f"src must be [sequences][at most {MAX_TREE}]")
+        n = src.size(1)
+        self._call("koala_kv4_move", _library().koala_kv4_move, B, at, stride, n, self._ints(src, (B, n), "src"), self._ints(dst, (B, n), "dst"),
+                   self._ints(status, (1,), "status"))
