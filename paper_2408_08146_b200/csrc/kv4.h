@@ -28,7 +28,11 @@ struct Kv4Attn {
   void *out_lo;                                 // KV4_PAIR: the residuals, laid out as `out`
   int q_type, out_type, n_heads;
   float scale;
+  unsigned long long g_inv;                     // div_inverse of the query heads per kv head (0: one); filled in by kv4_attention
+  __device__ __forceinline__ int by_group(int r) const { return g_inv == 0ull ? r : (int)div_by((unsigned)r, g_inv); }
+  float *scratch;                               // kv4_attention_scratch() bytes, 16-byte aligned
 };
+size_t kv4_attention_scratch(int dh, int num_sms, int rows);      // rows: of one kv head and sequence, at most
 cudaError_t kv4_attention(Launch L, int dh, const Kv4Attn &a, int num_sms);
 
 }  // namespace koala

@@ -6,10 +6,14 @@ using namespace koala;
 
 namespace {
 
+constexpr int NUM_SMS = 148;
+constexpr long long MAX_HEAD_ROWS = 1 << 19;      // (row, head) pairs of one sequence and kv head
+
 bool cache_ok(const koala_kv4 *k) {
   if (!k || k->struct_size != sizeof(koala_kv4)) return false;
   if (k->n_layers < 1 || k->n_kv_heads < 1 || k->n_kv_heads > 4096 || k->n_pages < 1 || (k->head_dim != 64 && k->head_dim != 128)) return false;
-  return k->page_size >= 16 && k->page_size <= 1024 && (k->page_size & (k->page_size - 1)) == 0;
+  if (k->page_size < 16 || k->page_size > 1024 || (k->page_size & (k->page_size - 1)) != 0) return false;
+  return (long long)k->n_pages * k->n_kv_heads <= (1ll << 31) / (k->page_size / KV4_G) - 1;      // granules of a layer are counted in 32 bits
 }
 bool pages_ok(const koala_kv4 *k) { return k->pages != nullptr && ((uintptr_t)k->pages & 127u) == 0; }
 
@@ -76,8 +80,10 @@ int koala_kv4_append(const koala_kv4 *k, int32_t layer, const koala_kv4_rows *r,
 }
 
 size_t koala_kv4_attention_scratch_bytes(const koala_kv4 *k, const koala_kv4_rows *r, int32_t n_heads) {
-  (void)k; (void)r; (void)n_heads;
-  return 0;
+  if (!cache_ok(k) || rows_ok(k, r) != KOALA_OK || n_heads < 1 || n_heads % k->n_kv_heads != 0 || r->total == 0 ||
+      (long long)r->max_rows * (n_heads / k->n_kv_heads) > MAX_HEAD_ROWS)
+    return 0;
+  return kv4_attention_scratch(k->head_dim, NUM_SMS, r->max_rows * (n_heads / k->n_kv_heads));
 }
 
 int koala_kv4_attention(const koala_kv4 *k, int32_t layer, const koala_kv4_rows *r, int32_t dtype, const koala_kv4_tensor *t, int32_t n_heads, float scale,
@@ -87,11 +93,13 @@ int koala_kv4_attention(const koala_kv4 *k, int32_t layer, const koala_kv4_rows 
   if (rc != KOALA_OK) return rc;
   if (!tensor_ok(t[0], dtype) || !tensor_ok(t[1], dtype)) return KOALA_E_INVALID;
   if (n_heads < 1 || n_heads > 65536 || n_heads % k->n_kv_heads != 0 || !(scale > 0.f && scale < 1e30f)) return KOALA_E_INVALID;
-  (void)scratch; (void)scratch_bytes;
+  if ((long long)r->max_rows * (n_heads / k->n_kv_heads) > MAX_HEAD_ROWS) return KOALA_E_UNSUPPORTED;
   if (r->total == 0) return KOALA_OK;
+  if (!scratch || scratch_bytes < koala_kv4_attention_scratch_bytes(k, r, n_heads)) return KOALA_E_CAPACITY;
+  if (((uintptr_t)scratch & 15u) != 0) return KOALA_E_INVALID;
   const Kv4Attn a{cache_of(k, r->page_table, r->table_stride), (size_t)layer * layer_bytes(k), rows_of(r), tensor_of(t[0]), tensor_of(t[1]), nullptr,
-                  dtype, dtype, n_heads, scale};
-  return done(kv4_attention(Launch{(cudaStream_t)cuda_stream, true}, k->head_dim, a, 148));
+                  dtype, dtype, n_heads, scale, 0ull, (float *)scratch};
+  return done(kv4_attention(Launch{(cudaStream_t)cuda_stream, true}, k->head_dim, a, NUM_SMS));
 }
 
 int koala_kv4_read(const koala_kv4 *k, int32_t layer, const koala_kv4_rows *r, int32_t dtype, const koala_kv4_tensor *t, const int64_t *layer_stride,

@@ -24,6 +24,9 @@
 #include "kv4.h"
 
 namespace koala {
+
+int kv4_attention_ctas(int num_sms, int nt);
+
 namespace {
 
 constexpr int WARPS = 4;
@@ -36,6 +39,14 @@ __device__ __forceinline__ void mma_f16(float *d, const uint32_t *a, uint32_t b0
       "{%0, %1, %2, %3};"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// the same with an accumulator of zeros
+__device__ __forceinline__ void mma_f16_first(float *d, const uint32_t *a, uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+      "{%10, %10, %10, %10};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
 }
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
   uint32_t d;
@@ -58,247 +69,426 @@ __device__ __forceinline__ uint32_t add2(uint32_t a, uint32_t b) {
   return *reinterpret_cast<const uint32_t *>(&h);
 }
 
-// element c of a row of q
-__device__ __forceinline__ float q_at(const void *p, int type, long long at) {
-  if (type == KV4_FP32) return reinterpret_cast<const float *>(p)[at];
-  if (type == KV4_BF16) return __bfloat162float(reinterpret_cast<const bf16 *>(p)[at]);
-  return __half2float(reinterpret_cast<const __half *>(p)[at]);
+// What a part (maximum, sum) counts relative to the maximum `top` over all parts; 0 for one that saw nothing.  (One that saw nothing
+// but NaN has no maximum either, but a NaN for a sum, which is taken in as it is.)
+__device__ __forceinline__ float share(float2 part, float top) { return part.x == -INFINITY ? 0.f : exp2f(part.x - top); }
+__device__ __forceinline__ void add4(float4 &v, float f, float4 x) {
+  if (f == 0.f) return;                                   // its numbers may be anything
+  v.x = fmaf(f, x.x, v.x); v.y = fmaf(f, x.y, v.y); v.z = fmaf(f, x.z, v.z); v.w = fmaf(f, x.w, v.w);
 }
-__device__ __forceinline__ void out_at(void *p, void *lo, int type, long long at, float v) {
-  if (type == KV4_FP32) reinterpret_cast<float *>(p)[at] = v;
-  else if (type == KV4_FP16) reinterpret_cast<__half *>(p)[at] = __float2half_rn(v);
-  else {
-    const bf16 hi = __float2bfloat16_rn(v);
-    reinterpret_cast<bf16 *>(p)[at] = hi;
-    if (type == KV4_PAIR && lo != nullptr) reinterpret_cast<bf16 *>(lo)[at] = __float2bfloat16_rn(v - __bfloat162float(hi));
+// dims d .. d + 3 of query row rr (of the rows that share kv head hk): v / sum
+__device__ __forceinline__ void finish(const Kv4Attn &A, int first, int hk, int G, int rr, int d, float4 v, float sum) {
+  const int i = A.by_group(rr);
+  const long long at = (long long)(first + i) * A.out.row + (long long)(hk * G + rr - i * G) * A.out.head + d;
+  // a row that sees nothing or is not in use is 0; one whose sum is NaN stays NaN
+  if (sum == 0.f || (A.rows.slot != nullptr && A.rows.slot[first + i] < 0)) v = make_float4(0.f, 0.f, 0.f, 0.f);
+  else v = make_float4(v.x / sum, v.y / sum, v.z / sum, v.w / sum);
+  if (A.out_type == KV4_FP32) {
+    *reinterpret_cast<float4 *>(reinterpret_cast<float *>(A.out.p) + at) = v;
+  } else if (A.out_type == KV4_FP16) {
+    *reinterpret_cast<uint2 *>(reinterpret_cast<__half *>(A.out.p) + at) = make_uint2(pack2(v.x, v.y), pack2(v.z, v.w));
+  } else {
+    const __nv_bfloat162 a = __floats2bfloat162_rn(v.x, v.y), b = __floats2bfloat162_rn(v.z, v.w);
+    *reinterpret_cast<uint2 *>(reinterpret_cast<bf16 *>(A.out.p) + at) = make_uint2(*reinterpret_cast<const uint32_t *>(&a), *reinterpret_cast<const uint32_t *>(&b));
+    if (A.out_type == KV4_PAIR && A.out_lo != nullptr) {
+      const float2 fa = __bfloat1622float2(a), fb = __bfloat1622float2(b);
+      const __nv_bfloat162 c = __floats2bfloat162_rn(v.x - fa.x, v.y - fa.y), e = __floats2bfloat162_rn(v.z - fb.x, v.w - fb.y);
+      *reinterpret_cast<uint2 *>(reinterpret_cast<bf16 *>(A.out_lo) + at) = make_uint2(*reinterpret_cast<const uint32_t *>(&c), *reinterpret_cast<const uint32_t *>(&e));
+    }
   }
 }
 
 // 2^k as a float, k within the range of normal numbers
 __device__ __forceinline__ float pow2i(int k) { return __int_as_float((k + 127) << 23); }
 
-__device__ __forceinline__ float ld_cluster(uint32_t local_addr, uint32_t rank) {
-  uint32_t ra;
-  float v;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(ra) : "r"(local_addr), "r"(rank));
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(ra) : "memory");
+__device__ __forceinline__ uint32_t smem_at(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void copy16(uint32_t dst, const void *src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ uint4 lds128(uint32_t at) {
+  uint4 v;
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
   return v;
 }
 
-template <int DH> struct Granule { uint4 k[DH / 64], v[DH / 64], p; };
+// The work of a launch as one line of units: for each sequence with rows, for each kv head and tile of its rows, one unit per
+// granule and START units for beginning (queries, first pages, the sums at the end).  CTA c of n takes units [U c / n, U (c + 1) / n).
+constexpr int START = 12;
+struct Sequence {
+  int first, count, ctx, kv, span, tiles;             // span: units of one head and tile
+  unsigned long long units;
+};
+template <int ROWS> __device__ __forceinline__ Sequence sequence(const Kv4Attn &A, int b, int G, bool tell) {
+  Sequence s;
+  s.first = s.count = s.ctx = s.kv = 0;
+  if (b < A.rows.B) {
+    A.rows.range(b, s.first, s.count);
+    s.ctx = A.rows.ctx_len[b];
+    s.kv = A.rows.kv_len != nullptr ? A.rows.kv_len[b] : s.ctx + s.count;
+    if (s.ctx < 0 || s.kv < 0) {
+      if (tell) A.rows.report();
+      s.ctx = s.kv = 0;
+    }
+    s.kv = min(s.kv, A.c.table_stride << (A.c.gpp_shift + 4));
+  }
+  s.span = START + (s.kv + KV4_G - 1) / KV4_G;
+  s.tiles = (s.count * G + ROWS - 1) / ROWS;
+  s.units = (unsigned long long)s.span * (unsigned)s.tiles * (unsigned)A.c.n_kv_heads;
+  return s;
+}
+__device__ __forceinline__ unsigned long long scan(unsigned long long v, int lane) {      // inclusive
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const unsigned long long x = __shfl_up_sync(0xffffffffu, v, o);
+    if (lane >= o) v += x;
+  }
+  return v;
+}
+// CTAs that share U units: each gets MIN_UNITS at least
+constexpr int MIN_UNITS = START + 8;
+__device__ __forceinline__ unsigned shares(unsigned long long U, unsigned grid) {
+  const unsigned long long n = (U + MIN_UNITS - 1) / MIN_UNITS;
+  return n < grid ? (unsigned)n : grid;
+}
+// a / b where a is mostly below 2^32
+__device__ __forceinline__ unsigned long long div64(unsigned long long a, unsigned b) {
+  return (a >> 32) == 0ull ? (unsigned long long)((unsigned)a / b) : a / b;
+}
+// floor(U c / n), c <= n <= 2^15
+__device__ __forceinline__ unsigned long long units_before(unsigned long long U, unsigned c, unsigned n) {
+  const unsigned long long q = div64(U, n);
+  return q * c + (unsigned)(U - q * n) * c / n;
+}
+__device__ __forceinline__ unsigned share_of(unsigned long long U, unsigned long long u, unsigned n) { return (unsigned)(((u + 1) * n - 1) / U); }
 
-// grid (chunks, row tiles, sequences * kv heads), clusters of `chunks` CTAs
+// A CTA's range begins inside at most one (head, tile) and ends inside at most one: two slots of partial sums, 0 for the
+// head or tile that an earlier CTA began, 1 for the one that a later CTA goes on with; [row][DH + 4]: O, maximum, sum.
+template <int DH> constexpr int SLOT_ROW = DH + 4;
+
+template <int NT> constexpr int DEPTH = NT == 1 ? 3 : 5;      // steps of a warp in its ring
+// Granules per step of a warp: two where registers allow, for independent instructions and half the bookkeeping.
+template <int NT> constexpr int STEP = NT == 1 ? 2 : 1;
+template <int DH, int NT> constexpr int RING = WARPS * DEPTH<NT> * STEP<NT> * kv4_granule_bytes(DH);
+
 template <int DH, int NT, bool PAIR>
-__global__ void __launch_bounds__(32 * WARPS) kv4_attn_kernel(const Kv4Attn A, int chunks) {
+__global__ void __launch_bounds__(32 * WARPS, NT == 1 ? 3 : 2) kv4_attn_kernel(const Kv4Attn A, float *__restrict__ scratch) {
   constexpr int KS = DH / 16;              // depth steps of S
   constexpr int MT = DH / 16;              // tiles of 16 dims of O
-  constexpr int ROWS = 8 * NT, OS = DH + 2;
-  __shared__ float part[WARPS][ROWS][OS];
-  __shared__ float mine[ROWS][OS];
-  pdl_launch_dependents();
+  constexpr int ROWS = 8 * NT, OS = DH + 4, GB = kv4_granule_bytes(DH), H = STEP<NT>, STAGES = DEPTH<NT>;
+  extern __shared__ __align__(128) unsigned char smem[];
+  static_assert(WARPS * ROWS * OS * 4 <= RING<DH, NT>, "the warps' sums go where the ring was");
+  float *part = reinterpret_cast<float *>(smem);          // [WARPS][ROWS][OS]
   pdl_wait();
+  pdl_launch_dependents();                 // in this order: the kernel that follows reads the plan before its own wait
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  const int chunk = blockIdx.x, hk = blockIdx.z % A.c.n_kv_heads, b = blockIdx.z / A.c.n_kv_heads;
   const int G = A.n_heads / A.c.n_kv_heads;
-  int first, count;
-  A.rows.range(b, first, count);
-  const int row0 = blockIdx.y * ROWS;      // of the count * G rows of this kv head
-  const int ctx = A.rows.ctx_len[b];
-  int kv = A.rows.kv_len != nullptr ? A.rows.kv_len[b] : ctx + count;
-  const bool bad = ctx < 0 || kv < 0;
-  if (bad && threadIdx.x == 0) A.rows.report();
-  kv = bad || row0 >= count * G ? 0 : min(kv, A.c.table_stride << (A.c.gpp_shift + 4));
-  const int granules = (kv + KV4_G - 1) / KV4_G;
-  const int lo = (int)((long long)granules * chunk / chunks), hi = (int)((long long)granules * (chunk + 1) / chunks);
-  const int cache_row = A.rows.cache_of(b);
-
-  // ---- this thread's two sets of rows: row g as a column of operand B (q), rows 2t and 2t + 1 as columns of the scores
-  uint32_t qf[PAIR ? 2 : 1][NT][KS][2];
-  float F[NT][2], Z[NT][2];
-  uint64_t m0[NT][2], m1[NT][2];
-  int last[NT][2];                         // slot up to which a row sees (no mask: its own); -2: not in use
-#pragma unroll
-  for (int n = 0; n < NT; ++n) {
-    const int r = row0 + 8 * n + g, i = r / G;
-    const bool in = r < count * G;
-    const long long at = in ? (long long)(first + i) * A.q.row + (long long)(hk * G + r % G) * A.q.head : 0;
-    float x[KS][4];
-    float top = 0.f, sum = 0.f;
-#pragma unroll
-    for (int s = 0; s < KS; ++s) {
-      // step s takes pairs 2 (s & 1) and 2 (s & 1) + 1 of the thread's word s / 2
-      const int d = 4 * (t * (DH / 32) + (s >> 1)) + 2 * (s & 1);
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        x[s][2 * e] = in ? q_at(A.q.p, A.q_type, at + d + e) : 0.f;
-        x[s][2 * e + 1] = in ? q_at(A.q.p, A.q_type, at + DH / 2 + d + e) : 0.f;
-      }
-#pragma unroll
-      for (int e = 0; e < 4; ++e) { top = fmaxf(top, fabsf(x[s][e])); sum += x[s][e]; }
-    }
-    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-    sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-    sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-    int ex = (int)(__float_as_uint(top) >> 23) - 127;       // 2^ex <= top < 2^(ex + 1)
-    ex = max(-112, min(ex, 126));                            // (rows of zeros; infinities stay infinities)
-    const float up = pow2i(14 - ex);
-#pragma unroll
-    for (int s = 0; s < KS; ++s)
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const float f = e == 0 ? up : up * 0.0625f;          // the second pair's codes come 16 times as large
-        const float y0 = x[s][2 * e] * f, y1 = x[s][2 * e + 1] * f;
-        qf[0][n][s][e] = pack2(y0, y1);
-        if constexpr (PAIR) {
-          const float2 h = unpack2(qf[0][n][s][e]);
-          qf[PAIR ? 1 : 0][n][s][e] = pack2(y0 - h.x, y1 - h.y);
-        }
-      }
-    const float scale = A.scale * 1.4426950408889634f;
-    const float f = fminf(scale * 16777216.f / up, 3e38f), z = sum * scale;
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      F[n][j] = __shfl_sync(0xffffffffu, f, (2 * t + j) * 4);
-      Z[n][j] = __shfl_sync(0xffffffffu, z, (2 * t + j) * 4);
-      const int rr = row0 + 8 * n + 2 * t + j, ii = rr / G;
-      const bool used = rr < count * G && !(A.rows.slot != nullptr && A.rows.slot[first + ii] < 0);
-      m0[n][j] = used && A.rows.mask != nullptr ? A.rows.mask[(size_t)(first + ii) * 2] : 0ull;
-      m1[n][j] = used && A.rows.mask != nullptr ? A.rows.mask[(size_t)(first + ii) * 2 + 1] : 0ull;
-      last[n][j] = !used ? -2 : A.rows.mask != nullptr ? ctx - 1 : ctx + ii;
-    }
-  }
   const bool tree = A.rows.mask != nullptr;
+  const uint32_t ring = smem_at(smem) + (uint32_t)(warp * STAGES * H * GB);
 
-  float o[NT][MT][4], mref[NT][2], mu[NT][2], l[NT][2], zs[NT][2];
+  // sequences `lane` stay in registers: most launches have no more
+  const Sequence near = sequence<ROWS>(A, lane, G, blockIdx.x == 0 && warp == 0);
+  unsigned long long U = near.units;
+  for (int j = 32; j < A.rows.B; j += 32) U += sequence<ROWS>(A, j + lane, G, blockIdx.x == 0 && warp == 0).units;
 #pragma unroll
-  for (int n = 0; n < NT; ++n) {
-#pragma unroll
-    for (int i = 0; i < MT; ++i) o[n][i][0] = o[n][i][1] = o[n][i][2] = o[n][i][3] = 0.f;
-#pragma unroll
-    for (int j = 0; j < 2; ++j) { mref[n][j] = -INFINITY; mu[n][j] = 0.f; l[n][j] = 0.f; zs[n][j] = 0.f; }
-  }
-  float C = pow2i(100);                    // power of two on the V scales, lowered as larger ones come
+  for (int o = 16; o > 0; o >>= 1) U += __shfl_xor_sync(0xffffffffu, U, o);
+  if (U == 0) return;
+  const unsigned n_shares = shares(U, gridDim.x);
+  if (blockIdx.x >= n_shares) return;
+  const unsigned long long u_end = units_before(U, blockIdx.x + 1, n_shares);
 
-  const unsigned char *base = A.c.pages + A.layer_off;
-  auto fetch = [&](int gi, Granule<DH> &f) -> bool {
-    const long long off = gi < hi ? A.c.granule<DH>(A.c.page_of(cache_row, gi), hk, gi) : -1;
-    if (off < 0) {
-      if (gi < hi && lane == 0) A.rows.report();
-      return false;
-    }
-    const unsigned char *p = base + off;
-#pragma unroll
-    for (int i = 0; i < DH / 64; ++i) {
-      f.k[i] = *reinterpret_cast<const uint4 *>(p + i * 512 + lane * 16);
-      f.v[i] = *reinterpret_cast<const uint4 *>(p + KV4_G * DH / 2 + i * 512 + lane * 16);
-    }
-    f.p = *reinterpret_cast<const uint4 *>(p + KV4_G * DH + g * 16);
-    return true;
-  };
-
-  Granule<DH> cur, nxt;
-  bool have = fetch(lo + warp, cur);
 #pragma unroll 1
-  for (int gi = lo + warp; gi < hi; gi += WARPS) {
-    const bool have_n = fetch(gi + WARPS, nxt);
-    if (have) {
-      const int key0 = gi * KV4_G;
-      // ---- S^T, two chains of accumulation
-      float acc[NT][2][4];
+  for (unsigned long long u = units_before(U, blockIdx.x, n_shares); u < u_end;) {
+    // ---- the sequence, head and tile of unit u
+    int b = 0;
+    unsigned long long before = 0;
+    Sequence sq;
+    for (int j = 0;; j += 32) {
+      const Sequence mine = j == 0 ? near : sequence<ROWS>(A, j + lane, G, false);
+      const unsigned long long upto = before + scan(mine.units, lane);
+      const unsigned hit = __ballot_sync(0xffffffffu, upto > u);
+      if (hit == 0u) { before = __shfl_sync(0xffffffffu, upto, 31); continue; }      // (some sequence has unit u)
+      const int at = __ffs(hit) - 1;
+      b = j + at;
+      sq.first = __shfl_sync(0xffffffffu, mine.first, at);
+      sq.count = __shfl_sync(0xffffffffu, mine.count, at);
+      sq.ctx = __shfl_sync(0xffffffffu, mine.ctx, at);
+      sq.kv = __shfl_sync(0xffffffffu, mine.kv, at);
+      sq.span = __shfl_sync(0xffffffffu, mine.span, at);
+      sq.tiles = __shfl_sync(0xffffffffu, mine.tiles, at);
+      before = __shfl_sync(0xffffffffu, upto - mine.units, at);
+      break;
+    }
+    const unsigned long long in_seq = u - before;
+    const unsigned item = (unsigned)div64(in_seq, (unsigned)sq.span);
+    const int from = (int)(in_seq - (unsigned long long)item * (unsigned)sq.span);
+    const int hk = (int)(item / (unsigned)sq.tiles), row0 = (int)(item - (unsigned)hk * (unsigned)sq.tiles) * ROWS;
+    const int to = (int)min((unsigned long long)sq.span, (unsigned long long)from + (u_end - u));
+    u += (unsigned)(to - from);
+    const int lo = max(0, from - START), hi = max(0, to - START);
+    const int first = sq.first, count = sq.count, ctx = sq.ctx, kv = min(sq.kv, hi * KV4_G);      // slots behind `hi` are another CTA's
+    const int n_rows = count * G;
+    const int cache_row = A.rows.cache_of(b);
+
+    // ---- this warp's steps of H granules: the warp-th, the one WARPS further, ..; the pages of 32 granules at a time
+    const int steps = hi - lo > H * warp ? (hi - lo - H * warp + H * WARPS - 1) / (H * WARPS) : 0;
+    const unsigned char *base = A.c.pages + A.layer_off;
+    auto granule_of = [&](int n) { return lo + ((n / H) * WARPS + warp) * H + n % H; };      // the warp's n-th granule
+    auto pages_from = [&](int n) {
+      const int gi = granule_of(n + lane);
+      if (gi >= hi) return -1;
+      const int page = A.c.page_of(cache_row, gi);
+      if ((unsigned)page >= (unsigned)A.c.n_pages) A.rows.report();
+      return page;
+    };
+    // bit h of have[stage]: granule h of the step in that stage is there
+    int page_now = pages_from(0), page_next = pages_from(32);
+    unsigned have = 0u;                    // two bits a step, the latest lowest
+    auto request = [&](int step) {         // in step order
+      if (step < steps) {
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
+        for (int h = 0; h < H; ++h) {
+          const int n = step * H + h, gi = granule_of(n);
+          const int page = __shfl_sync(0xffffffffu, page_now, n & 31);
+          const bool ok = (unsigned)page < (unsigned)A.c.n_pages;
+          have = have << 1 | (ok ? 1u : 0u);
+          if (ok) {
+            const uint32_t dst = ring + (uint32_t)((step % STAGES * H + h) * GB + lane * 16);
+            const unsigned char *src = base + A.c.granule<DH>(page, hk, gi) + lane * 16;
 #pragma unroll
-        for (int e = 0; e < 2; ++e) acc[n][e][0] = acc[n][e][1] = acc[n][e][2] = acc[n][e][3] = 0.f;
-#pragma unroll
-      for (int w = 0; w < KS / 2; ++w) {
-        uint32_t x, y;                     // word w of slots g and g + 8
-        if constexpr (DH == 128) {
-          x = (&cur.k[0].x)[w];
-          y = (&cur.k[DH / 64 - 1].x)[w];
-        } else {
-          x = (&cur.k[0].x)[w];
-          y = (&cur.k[0].x)[2 + w];
+            for (int i = 0; i < GB / 512; ++i) copy16(dst + i * 512, src + i * 512);
+            if (lane < (GB % 512) / 16) copy16(dst + GB / 512 * 512, src + GB / 512 * 512);
+          }
+          if ((n & 31) == 31) {            // the next 32 granules' pages
+            page_now = page_next;
+            page_next = pages_from(n + 33);
+          }
         }
+      } else {
+        have <<= H;
+      }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+#pragma unroll
+    for (int i = 0; i < STAGES - 1; ++i) request(i);
+
+    // ---- row g as a column of operand B (q), rows 2t and 2t + 1 as columns of the scores
+    uint32_t qf[PAIR ? 2 : 1][NT][KS][2];
+    float F[NT][2], Z[NT][2];              // score (base 2) = F (scaleK (q . code) + zeroK Z)
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const int r = row0 + 8 * n + g, i = A.by_group(r);
+      const bool in = r < n_rows;
+      const long long at = in ? (long long)(first + i) * A.q.row + (long long)(hk * G + r - i * G) * A.q.head : 0;
+      float x[KS][4];
+      float top = 0.f, sum = 0.f;
+      // the thread's word w covers dims d .. d + 3 and DH/2 + d ..: steps 2w and 2w + 1 take two pairs each
+      if constexpr (PAIR) {
+        float4 raw[KS];
+#pragma unroll
+        for (int w = 0; w < KS; ++w)
+          raw[w] = in ? *reinterpret_cast<const float4 *>(reinterpret_cast<const float *>(A.q.p) + at + (w & 1) * (DH / 2) + 4 * (t * (DH / 32) + (w >> 1)))
+                      : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int w = 0; w < KS; ++w) {
+          x[w & ~1][w & 1] = raw[w].x; x[w & ~1][2 + (w & 1)] = raw[w].y;
+          x[w | 1][w & 1] = raw[w].z; x[w | 1][2 + (w & 1)] = raw[w].w;
+        }
+      } else {
+        uint2 raw[KS];
+#pragma unroll
+        for (int w = 0; w < KS; ++w)
+          raw[w] = in ? *reinterpret_cast<const uint2 *>(reinterpret_cast<const __half *>(A.q.p) + at + (w & 1) * (DH / 2) + 4 * (t * (DH / 32) + (w >> 1)))
+                      : make_uint2(0u, 0u);
+        const bool is_bf16 = A.q_type == KV4_BF16;
+#pragma unroll
+        for (int w = 0; w < KS; ++w) {
+          const float2 a = is_bf16 ? make_float2(__uint_as_float(raw[w].x << 16), __uint_as_float(raw[w].x & 0xffff0000u)) : unpack2(raw[w].x);
+          const float2 c = is_bf16 ? make_float2(__uint_as_float(raw[w].y << 16), __uint_as_float(raw[w].y & 0xffff0000u)) : unpack2(raw[w].y);
+          x[w & ~1][w & 1] = a.x; x[w & ~1][2 + (w & 1)] = a.y;
+          x[w | 1][w & 1] = c.x; x[w | 1][2 + (w & 1)] = c.y;
+        }
+      }
+#pragma unroll
+      for (int s = 0; s < KS; ++s)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { top = fmaxf(top, fabsf(x[s][e])); sum += x[s][e]; }
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+      sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+      sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+      int ex = (int)(__float_as_uint(top) >> 23) - 127;     // 2^ex <= top < 2^(ex + 1)
+      ex = max(-112, min(ex, 126));                          // (rows of zeros; infinities stay infinities)
+      const float up = pow2i(14 - ex);
+#pragma unroll
+      for (int s = 0; s < KS; ++s)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          const uint32_t a[4] = {x & 0x000f000fu, y & 0x000f000fu, x & 0x00f000f0u, y & 0x00f000f0u};
-#pragma unroll
-          for (int n = 0; n < NT; ++n) {
-            mma_f16(acc[n][e], a, qf[0][n][2 * w + e][0], qf[0][n][2 * w + e][1]);
-            if constexpr (PAIR) mma_f16(acc[n][e], a, qf[PAIR ? 1 : 0][n][2 * w + e][0], qf[PAIR ? 1 : 0][n][2 * w + e][1]);
+          const float f = e == 0 ? up : up * 0.0625f;        // the second pair's codes come 16 times as large
+          const float y0 = x[s][2 * e] * f, y1 = x[s][2 * e + 1] * f;
+          qf[0][n][s][e] = pack2(y0, y1);
+          if constexpr (PAIR) {
+            const float2 h = unpack2(qf[0][n][s][e]);
+            qf[PAIR ? 1 : 0][n][s][e] = pack2(y0 - h.x, y1 - h.y);
           }
-          x >>= 8;
-          y >>= 8;
+        }
+      const float scale = A.scale * 1.4426950408889634f;
+      const float f = fminf(scale * 16777216.f / up, 3e38f), z = sum * (up * 5.9604644775390625e-8f);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        F[n][j] = __shfl_sync(0xffffffffu, f, (2 * t + j) * 4);
+        Z[n][j] = __shfl_sync(0xffffffffu, z, (2 * t + j) * 4);
+      }
+    }
+
+    float o[NT][MT][4], mref[NT][2], over[NT][2], mu[NT][2], l[NT][2], zs[NT][2];      // over: the score that raises the reference
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+#pragma unroll
+      for (int i = 0; i < MT; ++i) o[n][i][0] = o[n][i][1] = o[n][i][2] = o[n][i][3] = 0.f;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) { mref[n][j] = over[n][j] = -INFINITY; mu[n][j] = 0.f; l[n][j] = 0.f; zs[n][j] = 0.f; }
+    }
+    float C = pow2i(100);                  // power of two on the V scales, lowered as larger ones come
+
+#pragma unroll 1
+    for (int step = 0; step < steps; ++step) {
+      __syncwarp();                        // the stage asked for now was read in the previous step
+      request(step + STAGES - 1);
+      asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1) : "memory");
+      __syncwarp();
+      const unsigned there = have >> ((STAGES - 1) * H) & ((1u << H) - 1u);      // bit H - 1 - h: granule h
+      if (there == 0u) continue;
+      const uint32_t at = ring + (uint32_t)(step % STAGES * H * GB);
+      const int key0 = granule_of(step * H) * KV4_G;
+      // ---- S^T
+      float s[H][NT][4];
+      float sv[H][2], zv[H][2];
+      {
+        uint4 par[H];
+        uint32_t kx[H][KS / 2], ky[H][KS / 2];   // the words of slots g and g + 8
+#pragma unroll
+        for (int h = 0; h < H; ++h) {
+          const uint4 k0 = lds128(at + h * GB + lane * 16);
+          if constexpr (DH == 128) {
+            const uint4 k1 = lds128(at + h * GB + 512 + lane * 16);
+            kx[h][0] = k0.x; kx[h][1] = k0.y; kx[h][KS / 2 - 2] = k0.z; kx[h][KS / 2 - 1] = k0.w;
+            ky[h][0] = k1.x; ky[h][1] = k1.y; ky[h][KS / 2 - 2] = k1.z; ky[h][KS / 2 - 1] = k1.w;
+          } else {
+            kx[h][0] = k0.x; kx[h][1] = k0.y; ky[h][0] = k0.z; ky[h][1] = k0.w;
+          }
+          par[h] = lds128(at + h * GB + KV4_G * DH + g * 16);
+        }
+#pragma unroll
+        for (int w = 0; w < KS / 2; ++w)
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+#pragma unroll
+            for (int h = 0; h < H; ++h) {
+              const uint32_t x = e == 0 ? kx[h][w] : kx[h][w] >> 8, y = e == 0 ? ky[h][w] : ky[h][w] >> 8;
+              uint32_t a[4] = {x & 0x000f000fu, y & 0x000f000fu, x & 0x00f000f0u, y & 0x00f000f0u};
+              if constexpr (PAIR) {
+                a[0] = add2(a[0], 0x80088008u); a[1] = add2(a[1], 0x80088008u);
+                a[2] = add2(a[2], 0x80808080u); a[3] = add2(a[3], 0x80808080u);
+              }
+#pragma unroll
+              for (int n = 0; n < NT; ++n) {
+                const uint32_t *q = qf[0][n][2 * w + e];
+                if (w == 0 && e == 0) mma_f16_first(s[h][n], a, q[0], q[1]);
+                else mma_f16(s[h][n], a, q[0], q[1]);
+                if constexpr (PAIR) mma_f16(s[h][n], a, qf[PAIR ? 1 : 0][n][2 * w + e][0], qf[PAIR ? 1 : 0][n][2 * w + e][1]);
+              }
+            }
+        // ---- scores, in units of F: accumulator e is slot g + 8 (e >> 1), row 2t + (e & 1)
+#pragma unroll
+        for (int h = 0; h < H; ++h) {
+          const uint32_t pk[2] = {par[h].x, par[h].y}, pv[2] = {par[h].z, par[h].w};
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const float ks = __uint_as_float(pk[e] << 16);
+            float kz = __uint_as_float(pk[e] & 0xffff0000u);
+            if constexpr (PAIR) kz = fmaf(8.f, ks, kz);
+            sv[h][e] = __uint_as_float(pv[e] << 16);
+            zv[h][e] = fmaf(8.f, sv[h][e], __uint_as_float(pv[e] & 0xffff0000u));
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+              for (int j = 0; j < 2; ++j) s[h][n][2 * e + j] = fmaf(ks, s[h][n][2 * e + j], kz * Z[n][j]);
+          }
         }
       }
-      // ---- scores: accumulator e is slot g + 8 (e >> 1), row 2t + (e & 1)
-      const uint32_t pk[2] = {cur.p.x, cur.p.y}, pv[2] = {cur.p.z, cur.p.w};
-      float ks[2], kz[2], sv[2], zv[2];
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        ks[e] = __uint_as_float(pk[e] << 16); kz[e] = __uint_as_float(pk[e] & 0xffff0000u);
-        sv[e] = __uint_as_float(pv[e] << 16); zv[e] = fmaf(8.f, sv[e], __uint_as_float(pv[e] & 0xffff0000u));
-      }
-      float s[NT][4];
-#pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          s[n][e] = fmaf(ks[e >> 1], (acc[n][0][e] + acc[n][1][e]) * F[n][e & 1], kz[e >> 1] * Z[n][e & 1]);
-      const bool open = key0 + KV4_G <= min(ctx, kv);
-      unsigned seen = 0xffffffffu;         // bit 4 n + e
+      const bool open = key0 + H * KV4_G <= min(ctx, kv) && there == (1u << H) - 1u;
       if (!open) {
-        seen = 0u;
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int key = key0 + g + 8 * (e >> 1), rel = key - ctx, j = e & 1;
-            bool v = last[n][j] != -2;
-            if (rel >= 0) v = tree ? (rel < 64 ? (m0[n][j] >> rel) & 1ull : rel < 128 ? (m1[n][j] >> (rel - 64)) & 1ull : 0ull) != 0ull : key <= last[n][j];
-            if (key >= kv) v = false;
-            s[n][e] = v ? s[n][e] : -INFINITY;
-            seen |= v ? 1u << (4 * n + e) : 0u;
+        bool any[H][2] = {};               // slots g and g + 8: seen by one of this thread's rows
+#pragma unroll 1
+        for (int nj = 0; nj < 2 * NT; ++nj) {
+          const int n = nj >> 1, j = nj & 1, rr = row0 + 8 * n + 2 * t + j, ii = A.by_group(rr);
+          const bool used = rr < n_rows && !(A.rows.slot != nullptr && A.rows.slot[first + ii] < 0);
+          uint64_t m0 = 0ull, m1 = 0ull;
+          if (tree && used) {
+            m0 = A.rows.mask[(size_t)(first + ii) * 2];
+            m1 = A.rows.mask[(size_t)(first + ii) * 2 + 1];
           }
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {      // what no row sees may hold anything, NaN included
-          bool any = false;
+          for (int h = 0; h < H; ++h)
 #pragma unroll
-          for (int n = 0; n < NT; ++n) any = any || (seen >> (4 * n + 2 * e) & 3u) != 0u;
-          if (!any) { sv[e] = 0.f; zv[e] = 0.f; }
+            for (int e = 0; e < 2; ++e) {
+              const int key = key0 + h * KV4_G + g + 8 * e, rel = key - ctx;
+              bool v = used && key < kv && (there >> (H - 1 - h) & 1u) != 0u;
+              if (rel >= 0) v = v && (tree ? (rel < 64 ? (m0 >> rel) & 1ull : rel < 128 ? (m1 >> (rel - 64)) & 1ull : 0ull) != 0ull : rel <= ii);
+              any[h][e] = any[h][e] || v;
+              const bool nan = v && !(fabsf(zv[h][e]) < INFINITY);      // a value that is NaN: the row becomes NaN here, and the value counts as 0 below
+#pragma unroll
+              for (int nn = 0; nn < NT; ++nn)
+#pragma unroll
+                for (int jj = 0; jj < 2; ++jj)
+                  if (nn == n && jj == j) {
+                    s[h][nn][2 * e + jj] = v ? s[h][nn][2 * e + jj] : -INFINITY;
+                    if (nan) l[nn][jj] = NAN;
+                  }
+            }
         }
+#pragma unroll
+        for (int h = 0; h < H; ++h)
+#pragma unroll
+          for (int e = 0; e < 2; ++e)      // what no row sees may hold anything
+            if (!any[h][e] || !(fabsf(zv[h][e]) < INFINITY)) { sv[h][e] = 0.f; zv[h][e] = 0.f; }
       }
-      float svc[2] = {sv[0] * C, sv[1] * C};
-      bool raise = svc[0] > WEIGHT_TOP || svc[1] > WEIGHT_TOP;
+      float most = 0.f;
+#pragma unroll
+      for (int h = 0; h < H; ++h) most = fmaxf(most, fmaxf(sv[h][0], sv[h][1]));
+      bool raise = most * C > WEIGHT_TOP;
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) raise = raise || s[n][e] > mref[n][e & 1] + RAISE;
+        for (int j = 0; j < 2; ++j) {
+          float mx = fmaxf(s[0][n][j], s[0][n][2 + j]);
+          if (H == 2) mx = fmaxf(mx, fmaxf(s[H - 1][n][j], s[H - 1][n][2 + j]));
+          raise = raise || mx > over[n][j];
+        }
       if (__any_sync(0xffffffffu, raise)) {
-        float most = fmaxf(sv[0], sv[1]);
 #pragma unroll
-        for (int d = 4; d < 32; d <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
+        for (int d = 1; d < 32; d <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
         float less = 1.f;                  // uniform over the warp
         if (most * C > WEIGHT_TOP) {
-          const float to = pow2i(136 - (int)(__float_as_uint(most) >> 23));          // most * to in [2^9, 2^10)
-          less = to / C;
-          C = to;
-          svc[0] = sv[0] * C;
-          svc[1] = sv[1] * C;
+          const float to2 = pow2i(136 - (int)(__float_as_uint(most) >> 23));          // most * to2 in [2^9, 2^10)
+          less = to2 / C;
+          C = to2;
         }
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
           float f[2];
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
-            float mx = fmaxf(s[n][j], s[n][2 + j]);
+            float mx = fmaxf(s[0][n][j], s[0][n][2 + j]);
+            if (H == 2) mx = fmaxf(mx, fmaxf(s[H - 1][n][j], s[H - 1][n][2 + j]));
 #pragma unroll
             for (int d = 4; d < 32; d <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
             f[j] = 1.f;
             if (mx > mref[n][j]) {
-              f[j] = mref[n][j] == -INFINITY ? 0.f : ex2(mref[n][j] - mx);
-              mref[n][j] = mu[n][j] = mx;
+              f[j] = ex2((mref[n][j] - mx) * F[n][j]);       // 0 the first time
+              mref[n][j] = mx;
+              over[n][j] = mx + RAISE / F[n][j];
+              mu[n][j] = mx * F[n][j];
             }
             l[n][j] *= f[j];
             zs[n][j] *= f[j];
@@ -309,180 +499,238 @@ __global__ void __launch_bounds__(32 * WARPS) kv4_attn_kernel(const Kv4Attn A, i
         }
       }
       // ---- weights
-      uint32_t pb[PAIR ? 2 : 1][NT][2];
+      uint32_t pb[H][PAIR ? 2 : 1][NT][2];
 #pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        float w[4];
+      for (int h = 0; h < H; ++h)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float p = ex2(s[n][e] - mu[n][e & 1]);
-          const bool v = open || (seen >> (4 * n + e) & 1u) != 0u;
-          l[n][e & 1] += p;
-          zs[n][e & 1] += v ? p * zv[e >> 1] : 0.f;
-          w[e] = v ? p * svc[e >> 1] : 0.f;
-        }
+        for (int n = 0; n < NT; ++n) {
+          float w[4];
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const uint32_t h = pack2(w[2 * e], w[2 * e + 1]);
-          pb[0][n][e] = transpose8x8(h);
-          if constexpr (PAIR) {
-            const float2 back = unpack2(h);
-            pb[PAIR ? 1 : 0][n][e] = transpose8x8(pack2(w[2 * e] - back.x, w[2 * e + 1] - back.y));
+          for (int e = 0; e < 4; ++e) {
+            const float p = ex2(fmaf(s[h][n][e], F[n][e & 1], -mu[n][e & 1]));
+            l[n][e & 1] += p;
+            zs[n][e & 1] = fmaf(p, zv[h][e >> 1], zs[n][e & 1]);
+            w[e] = p * (sv[h][e >> 1] * C);
           }
-        }
-      }
-      // ---- O^T: lane (g, t) has words g * DH/64 .. of slots 2t, 2t + 1 (first plane or half) and 2t + 8, 2t + 9
 #pragma unroll
-      for (int w = 0; w < DH / 64; ++w) {
-        uint32_t a0, a1, b0, b1;           // slots 2t, 2t + 1, 2t + 8, 2t + 9
-        if constexpr (DH == 128) {
-          a0 = (&cur.v[0].x)[w]; a1 = (&cur.v[0].x)[2 + w];
-          b0 = (&cur.v[DH / 64 - 1].x)[w]; b1 = (&cur.v[DH / 64 - 1].x)[2 + w];
-        } else {
-          a0 = cur.v[0].x; a1 = cur.v[0].y; b0 = cur.v[0].z; b1 = cur.v[0].w;
-        }
-        uint32_t x = __byte_perm(a0, a1, 0x5410), xh = __byte_perm(a0, a1, 0x7632);      // two slots side by side: dims 4l .., DH/2 + 4l ..
-        uint32_t y = __byte_perm(b0, b1, 0x5410), yh = __byte_perm(b0, b1, 0x7632);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const uint32_t mask = (i & 1) ? 0x00f000f0u : 0x000f000fu, eight = (i & 1) ? 0x80808080u : 0x80088008u;      // -8 * 16, -8
-          const uint32_t a[4] = {add2(x & mask, eight), add2(xh & mask, eight), add2(y & mask, eight), add2(yh & mask, eight)};
-#pragma unroll
-          for (int n = 0; n < NT; ++n) {
+          for (int e = 0; e < 2; ++e) {
+            const uint32_t hi2 = pack2(w[2 * e], w[2 * e + 1]);
+            pb[h][0][n][e] = transpose8x8(hi2);
             if constexpr (PAIR) {
-              float d[4] = {0.f, 0.f, 0.f, 0.f};
-              mma_f16(d, a, pb[0][n][0], pb[0][n][1]);
-              mma_f16(d, a, pb[PAIR ? 1 : 0][n][0], pb[PAIR ? 1 : 0][n][1]);
-#pragma unroll
-              for (int e = 0; e < 4; ++e) o[n][4 * w + i][e] += d[e];
-            } else {
-              mma_f16(o[n][4 * w + i], a, pb[0][n][0], pb[0][n][1]);
+              const float2 back = unpack2(hi2);
+              pb[h][PAIR ? 1 : 0][n][e] = transpose8x8(pack2(w[2 * e] - back.x, w[2 * e + 1] - back.y));
             }
           }
-          if (i == 1) { x >>= 8; xh >>= 8; y >>= 8; yh >>= 8; }
+        }
+      // ---- O^T: lane (g, t) has words g * DH/64 .. of slots 2t, 2t + 1 (first plane or half) and 2t + 8, 2t + 9
+#pragma unroll
+      for (int h = 0; h < H; ++h) {
+        const uint32_t vat = at + h * GB + KV4_G * DH / 2 + lane * 16;
+        const uint4 v0 = lds128(vat), v1 = DH == 128 ? lds128(vat + 512) : v0;
+#pragma unroll
+        for (int w = 0; w < DH / 64; ++w) {
+          uint32_t a0, a1, b0, b1;         // slots 2t, 2t + 1, 2t + 8, 2t + 9
+          if constexpr (DH == 128) {
+            a0 = w == 0 ? v0.x : v0.y; a1 = w == 0 ? v0.z : v0.w;
+            b0 = w == 0 ? v1.x : v1.y; b1 = w == 0 ? v1.z : v1.w;
+          } else {
+            a0 = v0.x; a1 = v0.y; b0 = v0.z; b1 = v0.w;
+          }
+          uint32_t x = __byte_perm(a0, a1, 0x5410), xh = __byte_perm(a0, a1, 0x7632);      // two slots side by side: dims 4l .., DH/2 + 4l ..
+          uint32_t y = __byte_perm(b0, b1, 0x5410), yh = __byte_perm(b0, b1, 0x7632);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t mask = (i & 1) ? 0x00f000f0u : 0x000f000fu, eight = (i & 1) ? 0x80808080u : 0x80088008u;      // -8 * 16, -8
+            const uint32_t a[4] = {add2(x & mask, eight), add2(xh & mask, eight), add2(y & mask, eight), add2(yh & mask, eight)};
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+              if constexpr (PAIR) {
+                float d[4];
+                mma_f16_first(d, a, pb[h][0][n][0], pb[h][0][n][1]);
+                mma_f16(d, a, pb[h][PAIR ? 1 : 0][n][0], pb[h][PAIR ? 1 : 0][n][1]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[n][4 * w + i][e] += d[e];
+              } else {
+                mma_f16(o[n][4 * w + i], a, pb[h][0][n][0], pb[h][0][n][1]);
+              }
+            }
+            if (i == 1) { x >>= 8; xh >>= 8; y >>= 8; yh >>= 8; }
+          }
         }
       }
     }
-    cur = nxt;
-    have = have_n;
-  }
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    __syncthreads();                       // every warp is done with its ring
 
-  // ---- this warp's sums, in true units
-  const float back = 1.f / C;              // a power of two
+    // ---- this warp's sums, in true units
+    const float back = 1.f / C;            // a power of two
 #pragma unroll
-  for (int n = 0; n < NT; ++n) {
+    for (int n = 0; n < NT; ++n) {
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
+      for (int j = 0; j < 2; ++j) {
 #pragma unroll
-      for (int d = 4; d < 32; d <<= 1) {
-        l[n][j] += __shfl_xor_sync(0xffffffffu, l[n][j], d);
-        zs[n][j] += __shfl_xor_sync(0xffffffffu, zs[n][j], d);
-      }
-      float *to = part[warp][8 * n + 2 * t + j];
-#pragma unroll
-      for (int w = 0; w < DH / 64; ++w)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int d = 4 * (g * (DH / 64) + w) + i;
-          const float f = (i & 1) ? 1048576.f : 16777216.f;          // 2^24, less the 16 of the upper nibbles
-          to[d] = fmaf(o[n][4 * w + i][j] * f, back, zs[n][j]);
-          to[DH / 2 + d] = fmaf(o[n][4 * w + i][2 + j] * f, back, zs[n][j]);
+        for (int d = 4; d < 32; d <<= 1) {
+          l[n][j] += __shfl_xor_sync(0xffffffffu, l[n][j], d);
+          zs[n][j] += __shfl_xor_sync(0xffffffffu, zs[n][j], d);
         }
-      if (g == 0) { to[DH] = mref[n][j]; to[DH + 1] = l[n][j]; }
-    }
-  }
-  __syncthreads();
-  // ---- the warps together, then the chunks of the cluster
-  auto weight = [](float m, float top) { return m == -INFINITY ? 0.f : exp2f(m - top); };
-  auto finish = [&](int r, int d, float v, float sum) {
-    const int rr = row0 + r;
-    if (rr >= count * G) return;
-    const long long at = (long long)(first + rr / G) * A.out.row + (long long)(hk * G + rr % G) * A.out.head + d;
-    // a row that sees nothing or is not in use is 0; one whose sum is NaN stays NaN
-    const bool none = sum == 0.f || (A.rows.slot != nullptr && A.rows.slot[first + rr / G] < 0);
-    out_at(A.out.p, A.out_lo, A.out_type, at, none ? 0.f : v / sum);
-  };
-  for (int e = threadIdx.x; e < ROWS * DH; e += 32 * WARPS) {
-    const int r = e / DH, d = e - r * DH;
-    float top = -INFINITY, sum = 0.f, v = 0.f;
+        float *sums = part + (warp * ROWS + 8 * n + 2 * t + j) * OS;
 #pragma unroll
-    for (int w = 0; w < WARPS; ++w) top = fmaxf(top, part[w][r][DH]);
+        for (int w = 0; w < DH / 64; ++w) {
+          const int d = 4 * (g * (DH / 64) + w);
+          const float f[2] = {16777216.f * back, 1048576.f * back};      // 2^24, less the 16 of the upper nibbles
+          float x[4], y[4];
 #pragma unroll
-    for (int w = 0; w < WARPS; ++w) {
-      const float f = weight(part[w][r][DH], top);
-      if (f == 0.f && part[w][r][DH + 1] == 0.f) continue;
-      sum += f * part[w][r][DH + 1];
-      v += f * part[w][r][d];
-    }
-    if (chunks == 1) {
-      finish(r, d, v, sum);
-    } else {
-      mine[r][d] = v;
-      if (d == 0) { mine[r][DH] = top; mine[r][DH + 1] = sum; }
-    }
-  }
-  if (chunks == 1) return;
-  asm volatile("barrier.cluster.arrive.release;" ::: "memory");
-  asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
-  const int share = DH / chunks;
-  const uint32_t addr = (uint32_t)__cvta_generic_to_shared(&mine[0][0]);
-  for (int e = threadIdx.x; e < ROWS * share; e += 32 * WARPS) {
-    const int r = e / share, d = chunk * share + e % share;
-    float m[8], sm[8], v[8];
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      m[k] = -INFINITY; sm[k] = 0.f; v[k] = 0.f;
-      if (k < chunks) {
-        m[k] = ld_cluster(addr + (uint32_t)(r * OS + DH) * 4u, (uint32_t)k);
-        sm[k] = ld_cluster(addr + (uint32_t)(r * OS + DH + 1) * 4u, (uint32_t)k);
-        v[k] = ld_cluster(addr + (uint32_t)(r * OS + d) * 4u, (uint32_t)k);
+          for (int i = 0; i < 4; ++i) {
+            x[i] = fmaf(o[n][4 * w + i][j], f[i & 1], zs[n][j]);
+            y[i] = fmaf(o[n][4 * w + i][2 + j], f[i & 1], zs[n][j]);
+          }
+          *reinterpret_cast<float4 *>(sums + d) = make_float4(x[0], x[1], x[2], x[3]);
+          *reinterpret_cast<float4 *>(sums + DH / 2 + d) = make_float4(y[0], y[1], y[2], y[3]);
+        }
+        if (g == 0) *reinterpret_cast<float2 *>(sums + DH) = make_float2(mref[n][j] * F[n][j], l[n][j]);
       }
     }
-    float top = -INFINITY, sum = 0.f, x = 0.f;
+    __syncthreads();
+    // ---- the warps together: a result, or a partial sum.  32 WARPS / ROWS threads a row, four dims at a time
+    const bool whole = from == 0 && to == sq.span;
+    float *slot = scratch + (size_t)(2 * blockIdx.x + (from == 0 ? 1 : 0)) * ROWS * SLOT_ROW<DH>;
+    constexpr int PER = 32 * WARPS / ROWS;
+    const int r = threadIdx.x / PER, sub = threadIdx.x % PER;
+    if (r < min(ROWS, n_rows - row0)) {
+      float2 ml[WARPS];
+      float top = -INFINITY, sum = 0.f, f[WARPS];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) top = fmaxf(top, m[k]);
+      for (int w = 0; w < WARPS; ++w) {
+        ml[w] = *reinterpret_cast<const float2 *>(part + (w * ROWS + r) * OS + DH);
+        top = fmaxf(top, ml[w].x);
+      }
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {          // in chunk order
-      const float f = weight(m[k], top);
-      if (f == 0.f && sm[k] == 0.f) continue;
-      sum += f * sm[k];
-      x += f * v[k];
+      for (int w = 0; w < WARPS; ++w) {
+        f[w] = share(ml[w], top);
+        sum += ml[w].x == -INFINITY ? ml[w].y : f[w] * ml[w].y;
+      }
+#pragma unroll
+      for (int d = 4 * sub; d < DH; d += 4 * PER) {
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) add4(v, f[w], *reinterpret_cast<const float4 *>(part + (w * ROWS + r) * OS + d));
+        if (whole) finish(A, first, hk, G, row0 + r, d, v, sum);
+        else *reinterpret_cast<float4 *>(slot + r * SLOT_ROW<DH> + d) = v;
+      }
+      if (!whole && sub == 0) *reinterpret_cast<float2 *>(slot + r * SLOT_ROW<DH> + DH) = make_float2(top, sum);
     }
-    finish(r, d, x, sum);
+    __syncthreads();                       // the sums are read: the ring may be filled again
   }
-  // no CTA leaves while another may still read its sums
-  asm volatile("barrier.cluster.arrive.release;" ::: "memory");
-  asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
 }
 
-template <int DH, int NT, bool PAIR> cudaError_t go(Launch L, const Kv4Attn &a, int chunks) {
-  const int G = a.n_heads / a.c.n_kv_heads, tiles = (a.rows.max_rows * G + 8 * NT - 1) / (8 * NT);
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(chunks, tiles, a.rows.B * a.c.n_kv_heads);
-  cfg.blockDim = dim3(32 * WARPS);
-  cfg.stream = L.st;
-  cudaLaunchAttribute attr[2];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = L.pdl ? 1 : 0;
-  attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = chunks;
-  attr[1].val.clusterDim.y = 1;
-  attr[1].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = chunks > 1 ? 2 : 1;
-  ++g_launches;
-  return cudaLaunchKernelEx(&cfg, kv4_attn_kernel<DH, NT, PAIR>, a, chunks);
+// Joins what several CTAs have of one head and tile.  grid (sequences * kv heads, tiles, rows of a tile): JOINERS groups of DH / 4
+// threads take the partial sums in turn (all of a thread's on their way together: 74 of them per head for one sequence of eight
+// kv heads).
+constexpr int JOINERS = 16;
+template <int DH, int ROWS>
+__global__ void __launch_bounds__(DH / 4 * JOINERS) kv4_join_kernel(const Kv4Attn A, const float *__restrict__ scratch, unsigned grid) {
+  constexpr int LANES = DH / 4;
+  __shared__ float4 acc[JOINERS][LANES];
+  __shared__ float2 ml[JOINERS];
+  pdl_launch_dependents();
+  const int lane = threadIdx.x & 31;
+  const int G = A.n_heads / A.c.n_kv_heads, Hk = A.c.n_kv_heads;
+  const int b = blockIdx.x / Hk, hk = blockIdx.x - b * Hk, tile = blockIdx.y, r = blockIdx.z;
+  unsigned long long U = 0, before = 0;
+  for (int j = 0; j < A.rows.B; j += 32) {
+    const unsigned long long n = sequence<ROWS>(A, j + lane, G, false).units;
+    U += n;
+    before += j + lane < b ? n : 0ull;
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    U += __shfl_xor_sync(0xffffffffu, U, o);
+    before += __shfl_xor_sync(0xffffffffu, before, o);
+  }
+  const Sequence sq = sequence<ROWS>(A, b, G, false);
+  const int row = tile * ROWS + r;
+  pdl_wait();                              // by every block, whatever it has to do: the launch must not end before the one it joins
+  if (row >= sq.count * G) return;
+  const unsigned n_shares = shares(U, grid);
+  const unsigned long long u0 = before + (unsigned long long)(hk * sq.tiles + tile) * (unsigned)sq.span;
+  const unsigned c0 = share_of(U, u0, n_shares), c1 = share_of(U, u0 + (unsigned)sq.span - 1, n_shares);
+  if (c0 == c1) return;
+  const int grp = threadIdx.x / LANES, l = threadIdx.x % LANES;
+  float top = -INFINITY, sum = 0.f;
+  float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+  constexpr int BATCH = 6;
+  for (unsigned c = c0 + grp; c <= c1; c += BATCH * JOINERS) {
+    float2 q[BATCH];
+    float4 x[BATCH];
+#pragma unroll
+    for (int k = 0; k < BATCH; ++k) {
+      const unsigned ck = c + k * JOINERS;
+      q[k] = make_float2(-INFINITY, 0.f);
+      if (ck > c1) continue;
+      const float *p = scratch + ((size_t)(2 * ck + (ck == c0 ? 1 : 0)) * ROWS + r) * SLOT_ROW<DH>;
+      q[k] = *reinterpret_cast<const float2 *>(p + DH);
+      x[k] = *reinterpret_cast<const float4 *>(p + 4 * l);
+    }
+    float m = top;
+#pragma unroll
+    for (int k = 0; k < BATCH; ++k) m = fmaxf(m, q[k].x);
+    const float was = share(make_float2(top, 0.f), m);
+    sum = top == -INFINITY ? sum : sum * was;
+    v.x *= was; v.y *= was; v.z *= was; v.w *= was;
+    top = m;
+#pragma unroll
+    for (int k = 0; k < BATCH; ++k) {
+      const float f = share(q[k], m);
+      sum += q[k].x == -INFINITY ? q[k].y : f * q[k].y;
+      if (f != 0.f) add4(v, f, x[k]);
+    }
+  }
+  acc[grp][l] = v;
+  if (l == 0) ml[grp] = make_float2(top, sum);
+  __syncthreads();
+  if (threadIdx.x >= LANES) return;
+  top = -INFINITY;
+  sum = 0.f;
+  v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+  for (int k = 0; k < JOINERS; ++k) top = fmaxf(top, ml[k].x);
+#pragma unroll
+  for (int k = 0; k < JOINERS; ++k) {
+    const float f = share(ml[k], top);
+    sum += ml[k].x == -INFINITY ? ml[k].y : f * ml[k].y;
+    add4(v, f, acc[k][l]);
+  }
+  finish(A, sq.first, hk, G, row, 4 * l, v, sum);
+}
+
+template <int DH, int NT, bool PAIR> cudaError_t go(Launch L, const Kv4Attn &a, int num_sms) {
+  static SmemOptIn optin;
+  cudaError_t e = optin.ensure((const void *)kv4_attn_kernel<DH, NT, PAIR>, RING<DH, NT>);
+  if (e != cudaSuccess) return e;
+  const int G = a.n_heads / a.c.n_kv_heads, rows = a.rows.max_rows * G, tiles = (rows + 8 * NT - 1) / (8 * NT);
+  const int grid = kv4_attention_ctas(num_sms, NT);
+  e = launch_k(kv4_attn_kernel<DH, NT, PAIR>, dim3(grid), dim3(32 * WARPS), RING<DH, NT>, L.st, L.pdl, a, a.scratch);
+  if (e != cudaSuccess) return e;
+  return launch_k(kv4_join_kernel<DH, 8 * NT>, dim3(a.rows.B * a.c.n_kv_heads, tiles, rows < 8 * NT ? rows : 8 * NT), dim3(DH / 4 * JOINERS), 0, L.st, L.pdl, a,
+                  (const float *)a.scratch, (unsigned)grid);
 }
 
 }  // namespace
 
-cudaError_t kv4_attention(Launch L, int dh, const Kv4Attn &a, int num_sms) {
-  const int G = a.n_heads / a.c.n_kv_heads, rows = a.rows.max_rows * G;
+int kv4_attention_ctas(int num_sms, int nt) { return num_sms * (nt == 1 ? 3 : 2); }
+
+size_t kv4_attention_scratch(int dh, int num_sms, int rows) {
+  const int nt = rows > 8 ? 2 : 1;
+  return (size_t)kv4_attention_ctas(num_sms, nt) * 2 * (8 * nt) * (dh + 4) * sizeof(float);
+}
+
+cudaError_t kv4_attention(Launch L, int dh, const Kv4Attn &args, int num_sms) {
+  Kv4Attn a = args;
+  const int G = a.n_heads / a.c.n_kv_heads;
+  a.g_inv = G > 1 ? div_inverse((unsigned)G) : 0ull;
+  const int rows = a.rows.max_rows * G;
   const bool pair = a.q_type == KV4_FP32, wide = rows > 8;
-  const int tiles = (rows + (wide ? 15 : 7)) / (wide ? 16 : 8);
-  int chunks = 1;
-  while (chunks < 8 && (long long)2 * chunks * tiles * a.rows.B * a.c.n_kv_heads <= 3 * num_sms) chunks *= 2;
-#define KV4_GO(D, N) (pair ? go<D, N, true>(L, a, chunks) : go<D, N, false>(L, a, chunks))
+#define KV4_GO(D, N) (pair ? go<D, N, true>(L, a, num_sms) : go<D, N, false>(L, a, num_sms))
   if (dh == 128) return wide ? KV4_GO(128, 2) : KV4_GO(128, 1);
   return wide ? KV4_GO(64, 2) : KV4_GO(64, 1);
 #undef KV4_GO

@@ -10,7 +10,7 @@ from paper_2408_08146_b200 import KoalaError, PagedKV4
 from paper_2408_08146_b200 import kv4 as m
 from tests.kv4_reference import floor_bf16, quantise
 
-INVALID, UNSUPPORTED = 1, 2
+INVALID, UNSUPPORTED, CAPACITY = 1, 2, 3
 
 
 def cache_c(**kw):
@@ -96,6 +96,15 @@ def test_more_refusals():
     empty = rows_c(total=0, row_start=4096)
     assert append(cache_c(), empty) == 0 and attention(cache_c(), empty) == 0
     assert lib.koala_kv4_read(C.byref(cache_c()), 0, C.byref(empty), 1, tensors(GOOD, GOOD), None, None) == 0
+
+
+def test_scratch_of_the_attention():
+    lib = m._library()
+    n = lambda heads=4, **kw: int(lib.koala_kv4_attention_scratch_bytes(C.byref(cache_c()), C.byref(rows_c(**kw)), heads))
+    assert n() > 0 and n(total=0, row_start=4096) == 0 and n(heads=6) == 0 and n(B=0) == 0
+    call = lambda at, size: lib.koala_kv4_attention(C.byref(cache_c()), 0, C.byref(rows_c()), 1, tensors(GOOD, GOOD), 4, 0.1, at, size, None)
+    assert call(None, n()) == CAPACITY and call(4096, n() - 1) == CAPACITY and call(4100, n()) == INVALID
+    assert lib.koala_kv4_attention(C.byref(cache_c()), 0, C.byref(rows_c(max_rows=1 << 20, total=1, row_start=4096)), 1, tensors(GOOD, GOOD), 4, 0.1, 4096, 1 << 40, None) == UNSUPPORTED
 
 
 def test_the_binding_checks_its_tensors():
