@@ -32,6 +32,10 @@ struct Kv4Attn {
   __device__ __forceinline__ int by_group(int r) const { return g_inv == 0ull ? r : (int)div_by((unsigned)r, g_inv); }
   float *scratch;                               // kv4_attention_scratch() bytes, 16-byte aligned
 };
+// kv4_attn_tc.cu: from more than KV4_FEW_ROWS rows of a kv head and sequence on
+constexpr int KV4_FEW_ROWS = 16;
+size_t kv4_attention_tc_scratch(int dh, int num_sms);
+cudaError_t kv4_attention_tc(Launch L, int dh, const Kv4Attn &a, int num_sms);
 size_t kv4_attention_scratch(int dh, int num_sms, int rows);      // rows: of one kv head and sequence, at most
 cudaError_t kv4_attention(Launch L, int dh, const Kv4Attn &a, int num_sms);
 

@@ -19,9 +19,7 @@
 // result, an eighth of a bf16 one); with fp32 queries as two.  Everything else is fp32.
 // The softmax is online with a reference maximum that is raised only when a score exceeds it by more than 2^4: in the common
 // case a granule needs no shuffles but one vote.
-#include <cuda_fp16.h>
-
-#include "kv4.h"
+#include "kv4_work.cuh"
 
 namespace koala {
 
@@ -53,53 +51,10 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(v));
   return d;
 }
-__device__ __forceinline__ float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-__device__ __forceinline__ uint32_t pack2(float x, float y) {
-  const __half2 h = __floats2half2_rn(x, y);
-  return *reinterpret_cast<const uint32_t *>(&h);
-}
-__device__ __forceinline__ float2 unpack2(uint32_t v) { return __half22float2(*reinterpret_cast<const __half2 *>(&v)); }
-
 __device__ __forceinline__ uint32_t add2(uint32_t a, uint32_t b) {
   const __half2 h = __hadd2(*reinterpret_cast<const __half2 *>(&a), *reinterpret_cast<const __half2 *>(&b));
   return *reinterpret_cast<const uint32_t *>(&h);
 }
-
-// What a part (maximum, sum) counts relative to the maximum `top` over all parts; 0 for one that saw nothing.  (One that saw nothing
-// but NaN has no maximum either, but a NaN for a sum, which is taken in as it is.)
-__device__ __forceinline__ float share(float2 part, float top) { return part.x == -INFINITY ? 0.f : exp2f(part.x - top); }
-__device__ __forceinline__ void add4(float4 &v, float f, float4 x) {
-  if (f == 0.f) return;                                   // its numbers may be anything
-  v.x = fmaf(f, x.x, v.x); v.y = fmaf(f, x.y, v.y); v.z = fmaf(f, x.z, v.z); v.w = fmaf(f, x.w, v.w);
-}
-// dims d .. d + 3 of query row rr (of the rows that share kv head hk): v / sum
-__device__ __forceinline__ void finish(const Kv4Attn &A, int first, int hk, int G, int rr, int d, float4 v, float sum) {
-  const int i = A.by_group(rr);
-  const long long at = (long long)(first + i) * A.out.row + (long long)(hk * G + rr - i * G) * A.out.head + d;
-  // a row that sees nothing or is not in use is 0; one whose sum is NaN stays NaN
-  if (sum == 0.f || (A.rows.slot != nullptr && A.rows.slot[first + i] < 0)) v = make_float4(0.f, 0.f, 0.f, 0.f);
-  else v = make_float4(v.x / sum, v.y / sum, v.z / sum, v.w / sum);
-  if (A.out_type == KV4_FP32) {
-    *reinterpret_cast<float4 *>(reinterpret_cast<float *>(A.out.p) + at) = v;
-  } else if (A.out_type == KV4_FP16) {
-    *reinterpret_cast<uint2 *>(reinterpret_cast<__half *>(A.out.p) + at) = make_uint2(pack2(v.x, v.y), pack2(v.z, v.w));
-  } else {
-    const __nv_bfloat162 a = __floats2bfloat162_rn(v.x, v.y), b = __floats2bfloat162_rn(v.z, v.w);
-    *reinterpret_cast<uint2 *>(reinterpret_cast<bf16 *>(A.out.p) + at) = make_uint2(*reinterpret_cast<const uint32_t *>(&a), *reinterpret_cast<const uint32_t *>(&b));
-    if (A.out_type == KV4_PAIR && A.out_lo != nullptr) {
-      const float2 fa = __bfloat1622float2(a), fb = __bfloat1622float2(b);
-      const __nv_bfloat162 c = __floats2bfloat162_rn(v.x - fa.x, v.y - fa.y), e = __floats2bfloat162_rn(v.z - fb.x, v.w - fb.y);
-      *reinterpret_cast<uint2 *>(reinterpret_cast<bf16 *>(A.out_lo) + at) = make_uint2(*reinterpret_cast<const uint32_t *>(&c), *reinterpret_cast<const uint32_t *>(&e));
-    }
-  }
-}
-
-// 2^k as a float, k within the range of normal numbers
-__device__ __forceinline__ float pow2i(int k) { return __int_as_float((k + 127) << 23); }
 
 __device__ __forceinline__ uint32_t smem_at(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ void copy16(uint32_t dst, const void *src) {
@@ -111,67 +66,13 @@ __device__ __forceinline__ uint4 lds128(uint32_t at) {
   return v;
 }
 
-// The work of a launch as one line of units: for each sequence with rows, for each kv head and tile of its rows, one unit per
-// granule and START units for beginning (queries, first pages, the sums at the end).  CTA c of n takes units [U c / n, U (c + 1) / n).
-constexpr int START = 12;
-struct Sequence {
-  int first, count, ctx, kv, span, tiles;             // span: units of one head and tile
-  unsigned long long units;
-};
-template <int ROWS> __device__ __forceinline__ Sequence sequence(const Kv4Attn &A, int b, int G, bool tell) {
-  Sequence s;
-  s.first = s.count = s.ctx = s.kv = 0;
-  if (b < A.rows.B) {
-    A.rows.range(b, s.first, s.count);
-    s.ctx = A.rows.ctx_len[b];
-    s.kv = A.rows.kv_len != nullptr ? A.rows.kv_len[b] : s.ctx + s.count;
-    if (s.ctx < 0 || s.kv < 0) {
-      if (tell) A.rows.report();
-      s.ctx = s.kv = 0;
-    }
-    s.kv = min(s.kv, A.c.table_stride << (A.c.gpp_shift + 4));
-  }
-  s.span = START + (s.kv + KV4_G - 1) / KV4_G;
-  s.tiles = (s.count * G + ROWS - 1) / ROWS;
-  s.units = (unsigned long long)s.span * (unsigned)s.tiles * (unsigned)A.c.n_kv_heads;
-  return s;
-}
-__device__ __forceinline__ unsigned long long scan(unsigned long long v, int lane) {      // inclusive
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const unsigned long long x = __shfl_up_sync(0xffffffffu, v, o);
-    if (lane >= o) v += x;
-  }
-  return v;
-}
-// CTAs that share U units: each gets MIN_UNITS at least
-constexpr int MIN_UNITS = START + 8;
-__device__ __forceinline__ unsigned shares(unsigned long long U, unsigned grid) {
-  const unsigned long long n = (U + MIN_UNITS - 1) / MIN_UNITS;
-  return n < grid ? (unsigned)n : grid;
-}
-// a / b where a is mostly below 2^32
-__device__ __forceinline__ unsigned long long div64(unsigned long long a, unsigned b) {
-  return (a >> 32) == 0ull ? (unsigned long long)((unsigned)a / b) : a / b;
-}
-// floor(U c / n), c <= n <= 2^15
-__device__ __forceinline__ unsigned long long units_before(unsigned long long U, unsigned c, unsigned n) {
-  const unsigned long long q = div64(U, n);
-  return q * c + (unsigned)(U - q * n) * c / n;
-}
-__device__ __forceinline__ unsigned share_of(unsigned long long U, unsigned long long u, unsigned n) { return (unsigned)(((u + 1) * n - 1) / U); }
-
-// A CTA's range begins inside at most one (head, tile) and ends inside at most one: two slots of partial sums, 0 for the
-// head or tile that an earlier CTA began, 1 for the one that a later CTA goes on with; [row][DH + 4]: O, maximum, sum.
-template <int DH> constexpr int SLOT_ROW = DH + 4;
-
 template <int NT> constexpr int DEPTH = NT == 1 ? 3 : 5;      // steps of a warp in its ring
 // Granules per step of a warp: two where registers allow, for independent instructions and half the bookkeeping.
 template <int NT> constexpr int STEP = NT == 1 ? 2 : 1;
 template <int DH, int NT> constexpr int RING = WARPS * DEPTH<NT> * STEP<NT> * kv4_granule_bytes(DH);
 
 template <int DH, int NT, bool PAIR>
-__global__ void __launch_bounds__(32 * WARPS, NT == 1 ? 3 : 2) kv4_attn_kernel(const Kv4Attn A, float *__restrict__ scratch) {
+__global__ void __launch_bounds__(32 * WARPS, NT == 1 ? 3 : 2) kv4_attn_kernel(const Kv4Attn A, float *__restrict__ scratch, int tiles) {
   constexpr int KS = DH / 16;              // depth steps of S
   constexpr int MT = DH / 16;              // tiles of 16 dims of O
   constexpr int ROWS = 8 * NT, OS = DH + 4, GB = kv4_granule_bytes(DH), H = STEP<NT>, STAGES = DEPTH<NT>;
@@ -185,49 +86,15 @@ __global__ void __launch_bounds__(32 * WARPS, NT == 1 ? 3 : 2) kv4_attn_kernel(c
   const bool tree = A.rows.mask != nullptr;
   const uint32_t ring = smem_at(smem) + (uint32_t)(warp * STAGES * H * GB);
 
-  // sequences `lane` stay in registers: most launches have no more
-  const Sequence near = sequence<ROWS>(A, lane, G, blockIdx.x == 0 && warp == 0);
-  unsigned long long U = near.units;
-  for (int j = 32; j < A.rows.B; j += 32) U += sequence<ROWS>(A, j + lane, G, blockIdx.x == 0 && warp == 0).units;
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) U += __shfl_xor_sync(0xffffffffu, U, o);
-  if (U == 0) return;
-  const unsigned n_shares = shares(U, gridDim.x);
-  if (blockIdx.x >= n_shares) return;
-  const unsigned long long u_end = units_before(U, blockIdx.x + 1, n_shares);
-
+  Walk<ROWS, 1> walk;
+  if (!walk.begin(A, tiles, G, lane, blockIdx.x == 0 && warp == 0)) return;
+  Piece pc;
 #pragma unroll 1
-  for (unsigned long long u = units_before(U, blockIdx.x, n_shares); u < u_end;) {
-    // ---- the sequence, head and tile of unit u
-    int b = 0;
-    unsigned long long before = 0;
-    Sequence sq;
-    for (int j = 0;; j += 32) {
-      const Sequence mine = j == 0 ? near : sequence<ROWS>(A, j + lane, G, false);
-      const unsigned long long upto = before + scan(mine.units, lane);
-      const unsigned hit = __ballot_sync(0xffffffffu, upto > u);
-      if (hit == 0u) { before = __shfl_sync(0xffffffffu, upto, 31); continue; }      // (some sequence has unit u)
-      const int at = __ffs(hit) - 1;
-      b = j + at;
-      sq.first = __shfl_sync(0xffffffffu, mine.first, at);
-      sq.count = __shfl_sync(0xffffffffu, mine.count, at);
-      sq.ctx = __shfl_sync(0xffffffffu, mine.ctx, at);
-      sq.kv = __shfl_sync(0xffffffffu, mine.kv, at);
-      sq.span = __shfl_sync(0xffffffffu, mine.span, at);
-      sq.tiles = __shfl_sync(0xffffffffu, mine.tiles, at);
-      before = __shfl_sync(0xffffffffu, upto - mine.units, at);
-      break;
-    }
-    const unsigned long long in_seq = u - before;
-    const unsigned item = (unsigned)div64(in_seq, (unsigned)sq.span);
-    const int from = (int)(in_seq - (unsigned long long)item * (unsigned)sq.span);
-    const int hk = (int)(item / (unsigned)sq.tiles), row0 = (int)(item - (unsigned)hk * (unsigned)sq.tiles) * ROWS;
-    const int to = (int)min((unsigned long long)sq.span, (unsigned long long)from + (u_end - u));
-    u += (unsigned)(to - from);
-    const int lo = max(0, from - START), hi = max(0, to - START);
-    const int first = sq.first, count = sq.count, ctx = sq.ctx, kv = min(sq.kv, hi * KV4_G);      // slots behind `hi` are another CTA's
+  while (walk.next(A, G, lane, pc)) {
+    const int lo = pc.lo, hi = pc.hi, hk = pc.hk, row0 = pc.row0;
+    const int first = pc.first, count = pc.count, ctx = pc.ctx, kv = min(pc.kv, hi * KV4_G);      // slots behind `hi` are another CTA's
     const int n_rows = count * G;
-    const int cache_row = A.rows.cache_of(b);
+    const int cache_row = A.rows.cache_of(pc.b);
 
     // ---- this warp's steps of H granules: the warp-th, the one WARPS further, ..; the pages of 32 granules at a time
     const int steps = hi - lo > H * warp ? (hi - lo - H * warp + H * WARPS - 1) / (H * WARPS) : 0;
@@ -592,8 +459,7 @@ __global__ void __launch_bounds__(32 * WARPS, NT == 1 ? 3 : 2) kv4_attn_kernel(c
     }
     __syncthreads();
     // ---- the warps together: a result, or a partial sum.  32 WARPS / ROWS threads a row, four dims at a time
-    const bool whole = from == 0 && to == sq.span;
-    float *slot = scratch + (size_t)(2 * blockIdx.x + (from == 0 ? 1 : 0)) * ROWS * SLOT_ROW<DH>;
+    float *slot = part_of<DH, ROWS>(scratch, blockIdx.x, pc.begins);
     constexpr int PER = 32 * WARPS / ROWS;
     const int r = threadIdx.x / PER, sub = threadIdx.x % PER;
     if (r < min(ROWS, n_rows - row0)) {
@@ -614,93 +480,13 @@ __global__ void __launch_bounds__(32 * WARPS, NT == 1 ? 3 : 2) kv4_attn_kernel(c
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
         for (int w = 0; w < WARPS; ++w) add4(v, f[w], *reinterpret_cast<const float4 *>(part + (w * ROWS + r) * OS + d));
-        if (whole) finish(A, first, hk, G, row0 + r, d, v, sum);
-        else *reinterpret_cast<float4 *>(slot + r * SLOT_ROW<DH> + d) = v;
+        if (pc.whole) finish(A, first, hk, G, row0 + r, d, v, sum);
+        else *reinterpret_cast<float4 *>(slot + r * PART_ROW<DH> + d) = v;
       }
-      if (!whole && sub == 0) *reinterpret_cast<float2 *>(slot + r * SLOT_ROW<DH> + DH) = make_float2(top, sum);
+      if (!pc.whole && sub == 0) *reinterpret_cast<float2 *>(slot + r * PART_ROW<DH> + DH) = make_float2(top, sum);
     }
     __syncthreads();                       // the sums are read: the ring may be filled again
   }
-}
-
-// Joins what several CTAs have of one head and tile.  grid (sequences * kv heads, tiles, rows of a tile): JOINERS groups of DH / 4
-// threads take the partial sums in turn (all of a thread's on their way together: 74 of them per head for one sequence of eight
-// kv heads).
-constexpr int JOINERS = 16;
-template <int DH, int ROWS>
-__global__ void __launch_bounds__(DH / 4 * JOINERS) kv4_join_kernel(const Kv4Attn A, const float *__restrict__ scratch, unsigned grid) {
-  constexpr int LANES = DH / 4;
-  __shared__ float4 acc[JOINERS][LANES];
-  __shared__ float2 ml[JOINERS];
-  pdl_launch_dependents();
-  const int lane = threadIdx.x & 31;
-  const int G = A.n_heads / A.c.n_kv_heads, Hk = A.c.n_kv_heads;
-  const int b = blockIdx.x / Hk, hk = blockIdx.x - b * Hk, tile = blockIdx.y, r = blockIdx.z;
-  unsigned long long U = 0, before = 0;
-  for (int j = 0; j < A.rows.B; j += 32) {
-    const unsigned long long n = sequence<ROWS>(A, j + lane, G, false).units;
-    U += n;
-    before += j + lane < b ? n : 0ull;
-  }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    U += __shfl_xor_sync(0xffffffffu, U, o);
-    before += __shfl_xor_sync(0xffffffffu, before, o);
-  }
-  const Sequence sq = sequence<ROWS>(A, b, G, false);
-  const int row = tile * ROWS + r;
-  pdl_wait();                              // by every block, whatever it has to do: the launch must not end before the one it joins
-  if (row >= sq.count * G) return;
-  const unsigned n_shares = shares(U, grid);
-  const unsigned long long u0 = before + (unsigned long long)(hk * sq.tiles + tile) * (unsigned)sq.span;
-  const unsigned c0 = share_of(U, u0, n_shares), c1 = share_of(U, u0 + (unsigned)sq.span - 1, n_shares);
-  if (c0 == c1) return;
-  const int grp = threadIdx.x / LANES, l = threadIdx.x % LANES;
-  float top = -INFINITY, sum = 0.f;
-  float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-  constexpr int BATCH = 6;
-  for (unsigned c = c0 + grp; c <= c1; c += BATCH * JOINERS) {
-    float2 q[BATCH];
-    float4 x[BATCH];
-#pragma unroll
-    for (int k = 0; k < BATCH; ++k) {
-      const unsigned ck = c + k * JOINERS;
-      q[k] = make_float2(-INFINITY, 0.f);
-      if (ck > c1) continue;
-      const float *p = scratch + ((size_t)(2 * ck + (ck == c0 ? 1 : 0)) * ROWS + r) * SLOT_ROW<DH>;
-      q[k] = *reinterpret_cast<const float2 *>(p + DH);
-      x[k] = *reinterpret_cast<const float4 *>(p + 4 * l);
-    }
-    float m = top;
-#pragma unroll
-    for (int k = 0; k < BATCH; ++k) m = fmaxf(m, q[k].x);
-    const float was = share(make_float2(top, 0.f), m);
-    sum = top == -INFINITY ? sum : sum * was;
-    v.x *= was; v.y *= was; v.z *= was; v.w *= was;
-    top = m;
-#pragma unroll
-    for (int k = 0; k < BATCH; ++k) {
-      const float f = share(q[k], m);
-      sum += q[k].x == -INFINITY ? q[k].y : f * q[k].y;
-      if (f != 0.f) add4(v, f, x[k]);
-    }
-  }
-  acc[grp][l] = v;
-  if (l == 0) ml[grp] = make_float2(top, sum);
-  __syncthreads();
-  if (threadIdx.x >= LANES) return;
-  top = -INFINITY;
-  sum = 0.f;
-  v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-  for (int k = 0; k < JOINERS; ++k) top = fmaxf(top, ml[k].x);
-#pragma unroll
-  for (int k = 0; k < JOINERS; ++k) {
-    const float f = share(ml[k], top);
-    sum += ml[k].x == -INFINITY ? ml[k].y : f * ml[k].y;
-    add4(v, f, acc[k][l]);
-  }
-  finish(A, sq.first, hk, G, row, 4 * l, v, sum);
 }
 
 template <int DH, int NT, bool PAIR> cudaError_t go(Launch L, const Kv4Attn &a, int num_sms) {
@@ -709,10 +495,10 @@ template <int DH, int NT, bool PAIR> cudaError_t go(Launch L, const Kv4Attn &a, 
   if (e != cudaSuccess) return e;
   const int G = a.n_heads / a.c.n_kv_heads, rows = a.rows.max_rows * G, tiles = (rows + 8 * NT - 1) / (8 * NT);
   const int grid = kv4_attention_ctas(num_sms, NT);
-  e = launch_k(kv4_attn_kernel<DH, NT, PAIR>, dim3(grid), dim3(32 * WARPS), RING<DH, NT>, L.st, L.pdl, a, a.scratch);
+  e = launch_k(kv4_attn_kernel<DH, NT, PAIR>, dim3(grid), dim3(32 * WARPS), RING<DH, NT>, L.st, L.pdl, a, a.scratch, tiles);
   if (e != cudaSuccess) return e;
-  return launch_k(kv4_join_kernel<DH, 8 * NT>, dim3(a.rows.B * a.c.n_kv_heads, tiles, rows < 8 * NT ? rows : 8 * NT), dim3(DH / 4 * JOINERS), 0, L.st, L.pdl, a,
-                  (const float *)a.scratch, (unsigned)grid);
+  return launch_k(kv4_join_kernel<DH, 8 * NT, 1, 1, 16>, dim3(a.rows.B * tiles, a.c.n_kv_heads, rows < 8 * NT ? rows : 8 * NT), dim3(DH / 4 * 16), 0, L.st,
+                  L.pdl, a, a.scratch, tiles, (unsigned)grid);
 }
 
 }  // namespace
@@ -720,6 +506,7 @@ template <int DH, int NT, bool PAIR> cudaError_t go(Launch L, const Kv4Attn &a, 
 int kv4_attention_ctas(int num_sms, int nt) { return num_sms * (nt == 1 ? 3 : 2); }
 
 size_t kv4_attention_scratch(int dh, int num_sms, int rows) {
+  if (rows > KV4_FEW_ROWS) return kv4_attention_tc_scratch(dh, num_sms);
   const int nt = rows > 8 ? 2 : 1;
   return (size_t)kv4_attention_ctas(num_sms, nt) * 2 * (8 * nt) * (dh + 4) * sizeof(float);
 }
@@ -729,6 +516,7 @@ cudaError_t kv4_attention(Launch L, int dh, const Kv4Attn &args, int num_sms) {
   const int G = a.n_heads / a.c.n_kv_heads;
   a.g_inv = G > 1 ? div_inverse((unsigned)G) : 0ull;
   const int rows = a.rows.max_rows * G;
+  if (rows > KV4_FEW_ROWS) return kv4_attention_tc(L, dh, a, num_sms);
   const bool pair = a.q_type == KV4_FP32, wide = rows > 8;
 #define KV4_GO(D, N) (pair ? go<D, N, true>(L, a, num_sms) : go<D, N, false>(L, a, num_sms))
   if (dh == 128) return wide ? KV4_GO(128, 2) : KV4_GO(128, 1);

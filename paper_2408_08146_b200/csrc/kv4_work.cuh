@@ -1,0 +1,264 @@
+// How the attention kernels over the 4-bit cache deal their work to CTAs, and how parts of a result are joined.
+//
+// A head's rows are cut into tiles of ROWS (token, query head) pairs.  For each tile of each sequence and each kv head there is an
+// item: START units for beginning (queries, first pages, the sums at the end), and one unit for every UG granules of keys that some row of
+// the tile sees.  All units stand in one line, sequence by sequence, tile by tile, head by head; CTA c of n takes units [U c / n, U (c + 1) / n).  So
+// every CTA has the same work whatever the lengths, which only the device knows.  An item that lies in several CTAs leaves
+// parts (O, maximum, sum) that a second kernel joins in CTA order.
+#pragma once
+#include <cuda_fp16.h>
+
+#include "kv4.h"
+
+namespace koala {
+namespace {
+
+// START and the fewest units of a CTA are in units of UG granules
+template <int ROWS, int UG> struct Work {
+  static constexpr int START = UG == 1 ? 12 : 6;
+  static constexpr int MIN_UNITS = START + (UG == 1 ? 8 : 2);
+};
+
+struct Item {
+  int first, count, ctx, kv, span;                    // the sequence's rows; slots that the tile's rows may see; units
+};
+// tile `e % tiles` of sequence `e / tiles`
+template <int ROWS, int UG> __device__ __forceinline__ Item item_of(const Kv4Attn &A, int e, int tiles, int G, bool tell) {
+  Item s;
+  s.first = s.count = s.ctx = s.kv = s.span = 0;
+  const int b = tiles == 1 ? e : e / tiles, row0 = (e - b * tiles) * ROWS;
+  if (b >= A.rows.B) return s;
+  A.rows.range(b, s.first, s.count);
+  s.ctx = A.rows.ctx_len[b];
+  s.kv = A.rows.kv_len != nullptr ? A.rows.kv_len[b] : s.ctx + s.count;
+  if (s.ctx < 0 || s.kv < 0) {
+    if (tell) A.rows.report();
+    s.ctx = s.kv = 0;
+  }
+  s.kv = min(s.kv, A.c.table_stride << (A.c.gpp_shift + 4));
+  const int n_rows = s.count * G;
+  if (row0 >= n_rows) return s;
+  if (A.rows.mask == nullptr) s.kv = min(s.kv, s.ctx + A.by_group(min(row0 + ROWS, n_rows) - 1) + 1);
+  s.span = Work<ROWS, UG>::START + (s.kv + UG * KV4_G - 1) / (UG * KV4_G);
+  return s;
+}
+
+__device__ __forceinline__ unsigned long long scan(unsigned long long v, int lane) {      // inclusive
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const unsigned long long x = __shfl_up_sync(0xffffffffu, v, o);
+    if (lane >= o) v += x;
+  }
+  return v;
+}
+// a / b where a is mostly below 2^32
+__device__ __forceinline__ unsigned long long div64(unsigned long long a, unsigned b) {
+  return (a >> 32) == 0ull ? (unsigned long long)((unsigned)a / b) : a / b;
+}
+// floor(U c / n), c <= n <= 2^15
+__device__ __forceinline__ unsigned long long units_before(unsigned long long U, unsigned c, unsigned n) {
+  const unsigned long long q = div64(U, n);
+  return q * c + (unsigned)(U - q * n) * c / n;
+}
+// CTA that has unit u
+__device__ __forceinline__ unsigned cta_of(unsigned long long U, unsigned long long u, unsigned n) { return (unsigned)(((u + 1) * n - 1) / U); }
+template <int ROWS, int UG> __device__ __forceinline__ unsigned cta_count(unsigned long long U, unsigned grid) {
+  const unsigned long long n = (U + Work<ROWS, UG>::MIN_UNITS - 1) / Work<ROWS, UG>::MIN_UNITS;
+  return n < grid ? (unsigned)n : grid;
+}
+
+// A CTA's run of units, item by item; whole warps walk through it together.
+struct Piece {
+  int b, hk, row0, first, count, ctx, kv, lo, hi;     // keys: units lo .. hi - 1, of those the slots below kv
+  bool begins, whole;                                 // the item's first unit is this CTA's; all of them are
+};
+template <int ROWS, int UG> struct Walk {
+  unsigned long long u, end;
+  Item near;                                          // items 0 .. 31: most launches have no more
+  int entries, tiles;
+  // false: nothing to do for this CTA
+  __device__ __forceinline__ bool begin(const Kv4Attn &A, int n_tiles, int G, int lane, bool tell) {
+    tiles = n_tiles;
+    entries = A.rows.B * tiles;
+    const unsigned Hk = (unsigned)A.c.n_kv_heads;
+    near = item_of<ROWS, UG>(A, lane, tiles, G, tell);
+    unsigned long long U = (unsigned long long)(unsigned)near.span * Hk;
+    for (int j = 32; j < entries; j += 32) U += (unsigned long long)(unsigned)item_of<ROWS, UG>(A, j + lane, tiles, G, tell).span * Hk;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) U += __shfl_xor_sync(0xffffffffu, U, o);
+    if (U == 0) return false;
+    const unsigned n = cta_count<ROWS, UG>(U, gridDim.x);
+    if (blockIdx.x >= n) return false;
+    u = units_before(U, blockIdx.x, n);
+    end = units_before(U, blockIdx.x + 1, n);
+    return u < end;
+  }
+  __device__ __forceinline__ bool next(const Kv4Attn &A, int G, int lane, Piece &p) {
+    if (u >= end) return false;
+    const unsigned Hk = (unsigned)A.c.n_kv_heads;
+    unsigned long long before = 0;
+    for (int j = 0;; j += 32) {                       // (some item has unit u)
+      const Item it = j == 0 ? near : item_of<ROWS, UG>(A, j + lane, tiles, G, false);
+      const unsigned long long units = (unsigned long long)(unsigned)it.span * Hk, upto = before + scan(units, lane);
+      const unsigned hit = __ballot_sync(0xffffffffu, upto > u);
+      if (hit == 0u) {
+        before = __shfl_sync(0xffffffffu, upto, 31);
+        continue;
+      }
+      const int at = __ffs(hit) - 1, e = j + at;
+      p.b = tiles == 1 ? e : e / tiles;
+      p.row0 = (e - p.b * tiles) * ROWS;
+      p.first = __shfl_sync(0xffffffffu, it.first, at);
+      p.count = __shfl_sync(0xffffffffu, it.count, at);
+      p.ctx = __shfl_sync(0xffffffffu, it.ctx, at);
+      p.kv = __shfl_sync(0xffffffffu, it.kv, at);
+      const int span = __shfl_sync(0xffffffffu, it.span, at);
+      const unsigned long long in = u - __shfl_sync(0xffffffffu, upto - units, at);
+      p.hk = (int)div64(in, (unsigned)span);
+      const int from = (int)(in - (unsigned long long)(unsigned)p.hk * (unsigned)span);
+      const int to = (int)min((unsigned long long)span, (unsigned long long)from + (end - u));
+      u += (unsigned)(to - from);
+      p.lo = max(0, from - Work<ROWS, UG>::START);
+      p.hi = max(0, to - Work<ROWS, UG>::START);
+      p.begins = from == 0;
+      p.whole = from == 0 && to == span;
+      return true;
+    }
+  }
+};
+
+// Parts: two slots a CTA, 0 for the item that an earlier CTA began, 1 for the one that a later CTA goes on with; [row][DH + 4]: O, maximum, sum.
+template <int DH> constexpr int PART_ROW = DH + 4;
+template <int DH, int ROWS> __device__ __forceinline__ float *part_of(float *scratch, unsigned cta, bool begins) {
+  return scratch + (size_t)(2 * cta + (begins ? 1 : 0)) * ROWS * PART_ROW<DH>;
+}
+
+__device__ __forceinline__ uint32_t pack2(float x, float y) {
+  const __half2 h = __floats2half2_rn(x, y);
+  return *reinterpret_cast<const uint32_t *>(&h);
+}
+__device__ __forceinline__ float2 unpack2(uint32_t v) { return __half22float2(*reinterpret_cast<const __half2 *>(&v)); }
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// 2^k as a float, k within the range of normal numbers
+__device__ __forceinline__ float pow2i(int k) { return __int_as_float((k + 127) << 23); }
+
+// What a part (maximum, sum) counts relative to the maximum `top` over all parts; 0 for one that saw nothing.  (One that saw nothing
+// but NaN has no maximum either, but a NaN for a sum, which is taken in as it is.)
+__device__ __forceinline__ float share(float2 part, float top) { return part.x == -INFINITY ? 0.f : exp2f(part.x - top); }
+__device__ __forceinline__ void add4(float4 &v, float f, float4 x) {
+  if (f == 0.f) return;                                   // its numbers may be anything
+  v.x = fmaf(f, x.x, v.x); v.y = fmaf(f, x.y, v.y); v.z = fmaf(f, x.z, v.z); v.w = fmaf(f, x.w, v.w);
+}
+// dims d .. d + 3 of query row rr (of the rows that share kv head hk): v / sum
+__device__ __forceinline__ void finish(const Kv4Attn &A, int first, int hk, int G, int rr, int d, float4 v, float sum) {
+  const int i = A.by_group(rr);
+  const long long at = (long long)(first + i) * A.out.row + (long long)(hk * G + rr - i * G) * A.out.head + d;
+  // a row that sees nothing or is not in use is 0; one whose sum is NaN stays NaN
+  if (sum == 0.f || (A.rows.slot != nullptr && A.rows.slot[first + i] < 0)) v = make_float4(0.f, 0.f, 0.f, 0.f);
+  else v = make_float4(v.x / sum, v.y / sum, v.z / sum, v.w / sum);
+  if (A.out_type == KV4_FP32) {
+    *reinterpret_cast<float4 *>(reinterpret_cast<float *>(A.out.p) + at) = v;
+  } else if (A.out_type == KV4_FP16) {
+    *reinterpret_cast<uint2 *>(reinterpret_cast<__half *>(A.out.p) + at) = make_uint2(pack2(v.x, v.y), pack2(v.z, v.w));
+  } else {
+    const __nv_bfloat162 a = __floats2bfloat162_rn(v.x, v.y), b = __floats2bfloat162_rn(v.z, v.w);
+    *reinterpret_cast<uint2 *>(reinterpret_cast<bf16 *>(A.out.p) + at) = make_uint2(*reinterpret_cast<const uint32_t *>(&a), *reinterpret_cast<const uint32_t *>(&b));
+    if (A.out_type == KV4_PAIR && A.out_lo != nullptr) {
+      const float2 fa = __bfloat1622float2(a), fb = __bfloat1622float2(b);
+      const __nv_bfloat162 c = __floats2bfloat162_rn(v.x - fa.x, v.y - fa.y), e = __floats2bfloat162_rn(v.z - fb.x, v.w - fb.y);
+      *reinterpret_cast<uint2 *>(reinterpret_cast<bf16 *>(A.out_lo) + at) = make_uint2(*reinterpret_cast<const uint32_t *>(&c), *reinterpret_cast<const uint32_t *>(&e));
+    }
+  }
+}
+
+// Joins the parts of one item.  grid (sequences * tiles, kv heads, blocks of a tile's rows): RB rows a block, JOINERS groups of DH / 4
+// threads a row that take its parts in turn, BATCH at a time on their way together.
+template <int DH, int ROWS, int UG, int RB, int JOINERS>
+__global__ void __launch_bounds__(DH / 4 * JOINERS * RB) kv4_join_kernel(const Kv4Attn A, float *scratch, int tiles, unsigned grid) {
+  constexpr int LANES = DH / 4, BATCH = 5;
+  __shared__ float4 acc[RB][JOINERS][LANES];
+  __shared__ float2 ml[RB][JOINERS];
+  pdl_launch_dependents();
+  const int lane = threadIdx.x & 31, G = A.n_heads / A.c.n_kv_heads;
+  const unsigned Hk = (unsigned)A.c.n_kv_heads;
+  const int e = blockIdx.x, hk = blockIdx.y;
+  unsigned long long U = 0, before = 0;
+  Item it;
+  it.span = 0;
+  for (int j = 0; j < A.rows.B * tiles; j += 32) {
+    const Item x = item_of<ROWS, UG>(A, j + lane, tiles, G, false);
+    const unsigned long long n = (unsigned long long)(unsigned)x.span * Hk;
+    U += n;
+    before += j + lane < e ? n : 0ull;
+    if (e >= j && e < j + 32) {
+      it.first = __shfl_sync(0xffffffffu, x.first, e - j);
+      it.count = __shfl_sync(0xffffffffu, x.count, e - j);
+      it.span = __shfl_sync(0xffffffffu, x.span, e - j);
+    }
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    U += __shfl_xor_sync(0xffffffffu, U, o);
+    before += __shfl_xor_sync(0xffffffffu, before, o);
+  }
+  pdl_wait();                              // by every block, whatever it has to do: the launch must not end before the one it joins
+  if (it.span == 0) return;
+  const unsigned n = cta_count<ROWS, UG>(U, grid);
+  const unsigned long long u0 = before + (unsigned long long)(unsigned)hk * (unsigned)it.span;
+  const unsigned c0 = cta_of(U, u0, n), c1 = cta_of(U, u0 + (unsigned)it.span - 1, n);
+  if (c0 == c1) return;
+  const int l = threadIdx.x % LANES, grp = threadIdx.x / LANES % JOINERS, rb = threadIdx.x / (LANES * JOINERS);
+  const int r = blockIdx.z * RB + rb, row = (tiles == 1 ? 0 : e % tiles) * ROWS + r;
+  const bool in = row < it.count * G;
+  float top = -INFINITY, sum = 0.f;
+  float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (unsigned c = c0 + grp; in && c <= c1; c += BATCH * JOINERS) {
+    float2 q[BATCH];
+    float4 x[BATCH];
+#pragma unroll
+    for (int k = 0; k < BATCH; ++k) {
+      const unsigned ck = c + k * JOINERS;
+      q[k] = make_float2(-INFINITY, 0.f);
+      if (ck > c1) continue;
+      const float *p = part_of<DH, ROWS>(scratch, ck, ck == c0) + r * PART_ROW<DH>;
+      q[k] = *reinterpret_cast<const float2 *>(p + DH);
+      x[k] = *reinterpret_cast<const float4 *>(p + 4 * l);
+    }
+    float m = top;
+#pragma unroll
+    for (int k = 0; k < BATCH; ++k) m = fmaxf(m, q[k].x);
+    const float was = share(make_float2(top, 0.f), m);
+    sum = top == -INFINITY ? sum : sum * was;
+    v.x *= was; v.y *= was; v.z *= was; v.w *= was;
+    top = m;
+#pragma unroll
+    for (int k = 0; k < BATCH; ++k) {
+      const float f = share(q[k], m);
+      sum += q[k].x == -INFINITY ? q[k].y : f * q[k].y;
+      if (f != 0.f) add4(v, f, x[k]);
+    }
+  }
+  acc[rb][grp][l] = v;
+  if (l == 0) ml[rb][grp] = make_float2(top, sum);
+  __syncthreads();
+  if (grp != 0 || !in) return;
+  top = -INFINITY;
+  sum = 0.f;
+  v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+  for (int k = 0; k < JOINERS; ++k) top = fmaxf(top, ml[rb][k].x);
+#pragma unroll
+  for (int k = 0; k < JOINERS; ++k) {
+    const float f = share(ml[rb][k], top);
+    sum += ml[rb][k].x == -INFINITY ? ml[rb][k].y : f * ml[rb][k].y;
+    add4(v, f, acc[rb][k][l]);
+  }
+  finish(A, it.first, hk, G, row, 4 * l, v, sum);
+}
+
+}  // namespace
+}  // namespace koala

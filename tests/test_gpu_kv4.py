@@ -243,6 +243,10 @@ ATTENTION = [
     (1, 1, 128, 16, [16000], [1], "fp16", False),
     (2, 2, 128, 64, [5000], [33], "bf16", True),
     (40, 40, 128, 16, [95, 300, 64, 8], [18, 18, 18, 18], "bf16", True),
+    (4, 4, 64, 16, [200, 3], [20, 50], "bf16", True),
+    (6, 2, 64, 32, [129], [31], "fp32", True),
+    (4, 4, 64, 64, [1000], [40], "fp16", False),
+    (1, 1, 64, 16, [0, 63, 64, 65], [17, 17, 1, 64], "fp32", False),
 ]
 
 
