@@ -2,9 +2,11 @@
 //
 // One CTA per SM walks through its share of the work (kv4_work.cuh): tiles of 128 (token, head) rows of one kv head, keys in tiles
 // of 64.  Per key tile
-//   eight warps expand the codes of K (four) and V (four): shared memory, fp16, in the layouts that the MMAs read
+//   seven warps take the tiles' granules of 16 keys in turn and expand their codes: shared memory, fp16, in the layouts that
+//                            the MMAs read
 //   S[128 x 64]   = Q K^T    tcgen05.mma, A = Q and B = K from tensor and shared memory
-//   P             = 2^(...)  four warps, a thread per row; P goes where S was, in tensor memory
+//   P             = 2^(...)  four warps, a thread per row; P goes where S was, in tensor memory.  Two groups of four take
+//                            the tiles in turn, each with a maximum, a sum and an O of its own, joined at the end
 //   O[128 x DH]  += P V      tcgen05.mma, A = P from tensor memory, B = V as [key][dim] (MN-major)
 // With x = zero + scale code = (zero + 8 scale) + scale (code - 8): scale (code - 8) times a power of two is EXACT in fp16 (8 bits by 3),
 // so K and V are expanded without rounding, and the constants of the vectors come in as more columns of the products: four
@@ -27,15 +29,15 @@ namespace {
 constexpr int TK = 64;                     // keys of a tile
 constexpr int UG = TK / KV4_G;             // granules of a tile
 constexpr int NB = 3;                      // buffers of K and of V
-constexpr int RING = 4;                    // tiles of codes on their way per expanding warp
-constexpr int INFO = 8;                    // tiles whose powers of two are kept (expanding runs at most NB + 2 tiles ahead of the rows)
+constexpr int RING = 3;                    // granules on their way per expanding warp
+constexpr int INFO = 8;                    // tiles whose powers of two are kept (expanding runs at most NB + 3 tiles ahead of the rows)
 constexpr int BLK = TK * 128;              // [64 keys][64 dims]
-constexpr int ROW_WARPS = 4, EXPANDERS = 8, MMA_WARP = ROW_WARPS + EXPANDERS;
-constexpr int THREADS = 32 * (MMA_WARP + 1);
+constexpr int ROW_WARPS = 8, EXPANDERS = 7, MMA_WARP = ROW_WARPS + EXPANDERS;
+constexpr int THREADS = 32 * (MMA_WARP + 1);        // sixteen warps: 128 registers a thread
 constexpr int E_TIMEOUT = 6;
 constexpr float RAISE = 4.f;
 constexpr int P_TOP = 10;                  // P = 2^P_TOP at the reference maximum
-constexpr int COL_S = 0, COL_O = 2 * TK, COL_Q = COL_O + 144;
+constexpr int COL_S = 0, COL_O = 2 * TK, O_COLS = 144, COL_Q = COL_O + 2 * O_COLS;
 constexpr int TMEM_COLS = 512;
 
 enum { FULL = 0, HALF = 1, PAIR = 2 };     // 128 rows; 64 rows twice; 64 rows as two values
@@ -44,8 +46,9 @@ template <int DH> struct Lay {
   static constexpr int NBLK = DH / 64 + 1;                   // blocks of 64 dims, and the constants
   static constexpr int ONE = NBLK * BLK;
   static constexpr int K = 0, V = NB * ONE, CODES = 2 * NB * ONE;
-  static constexpr int PART = KV4_G * DH / 2 + KV4_PARAMS;   // what an expanding warp fetches per tile: a granule's K or V and its parameters
-  static constexpr int BYTES = CODES + EXPANDERS * RING * PART;
+  static constexpr int PART = kv4_granule_bytes(DH);
+  static constexpr int Q = CODES + EXPANDERS * RING * PART;  // rows of queries as they come: 128 of 16 bits, or 64 of 32
+  static constexpr int BYTES = Q + 128 * DH * 2;
 };
 template <int DH> constexpr unsigned SMEM = Lay<DH>::BYTES + 1024;
 
@@ -55,10 +58,11 @@ struct TileInfo {
   unsigned poison[UG], poison_v[UG];       // slots whose K / V is NaN
 };
 struct alignas(16) Sync {
-  uint64_t q_full, k_full[NB], k_empty[NB], v_full[NB], v_empty[NB], s_full[2], p_full[2], pv_done[2], info_full[INFO], drain;
+  uint64_t q_in, q_full, k_full[NB], k_empty[NB], v_full[NB], v_empty[NB], s_full[2], p_full[2], pv_done[2], info_full[INFO], x_full, x_empty, drain;
   uint32_t tmem;
   int error;
   TileInfo info[INFO];
+  float4 x[2][128];                        // the groups' maximum, sum and power of two of each row
 };
 
 __device__ __forceinline__ void arrive(uint64_t *bar) {
@@ -68,14 +72,35 @@ __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::be
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-// A from tensor memory
-__device__ __forceinline__ void umma_ts(uint32_t d, uint32_t a, uint64_t db, uint32_t idesc, uint32_t accumulate) {
+__device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t *v) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]) : "r"(taddr) : "memory");
+}
+// A from tensor memory.  The whole warp comes here and one lane (`leader`) issues: in a branch that one lane takes, the descriptors would be
+// worked out lane by lane and moved to the uniform registers that the instruction reads, some ten dependent instructions per MMA.
+__device__ __forceinline__ void umma_ts(uint32_t leader, uint32_t d, uint32_t a, uint64_t db, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\t"
+      "{\n\t.reg .pred p, q;\n\t"
       "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-      ::"r"(d), "r"(a), "l"(db), "r"(idesc), "r"(accumulate)
+      "setp.ne.b32 q, %5, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+      ::"r"(d), "r"(a), "l"(db), "r"(idesc), "r"(accumulate), "r"(leader)
       : "memory");
+}
+__device__ __forceinline__ void commit(uint32_t leader, uint64_t *bar) {
+  asm volatile(
+      "{\n\t.reg .pred q;\n\t"
+      "setp.ne.b32 q, %1, 0;\n\t"
+      "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(smem_u32(bar)), "r"(leader)
+      : "memory");
+}
+__device__ __forceinline__ void copy8(uint32_t dst, const void *src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ uint2 lds64(uint32_t at) {
+  uint2 v;
+  asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at) : "memory");
+  return v;
 }
 __device__ __forceinline__ void copy16(uint32_t dst, const void *src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
@@ -103,6 +128,39 @@ __device__ __forceinline__ void expand(uint32_t w, __half2 scale, uint32_t *x) {
   }
 }
 
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+// two floats at a time
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 both(float x, float y) {
+  f32x2 d;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(x), "f"(y));
+  return d;
+}
+__device__ __forceinline__ float2 apart(f32x2 v) {
+  float2 d;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(d.x), "=f"(d.y) : "l"(v));
+  return d;
+}
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
+  f32x2 d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
+  f32x2 d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
+  f32x2 d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+
 // rows of a tile of 64 keys that a row sees: bit j is key0 + j
 __device__ __forceinline__ uint64_t ones_below(int n) { return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1ull; }
 __device__ __forceinline__ uint64_t tree_bits(uint64_t m0, uint64_t m1, int shift) {      // shift = key0 - ctx
@@ -127,13 +185,16 @@ __global__ void __launch_bounds__(THREADS, 1) kv4_attn_tc_kernel(const Kv4Attn A
   const bool tree = A.rows.mask != nullptr;
 
   if (threadIdx.x == 0) {
+    mbar_init(&sync.q_in, ROW_WARPS);
     mbar_init(&sync.q_full, ROW_WARPS);
     for (int i = 0; i < NB; ++i) {
-      mbar_init(&sync.k_full[i], EXPANDERS / 2); mbar_init(&sync.k_empty[i], 1);
-      mbar_init(&sync.v_full[i], EXPANDERS / 2); mbar_init(&sync.v_empty[i], 1);
+      mbar_init(&sync.k_full[i], UG); mbar_init(&sync.k_empty[i], 1);
+      mbar_init(&sync.v_full[i], UG); mbar_init(&sync.v_empty[i], 1);
     }
-    for (int i = 0; i < 2; ++i) { mbar_init(&sync.s_full[i], 1); mbar_init(&sync.p_full[i], ROW_WARPS); mbar_init(&sync.pv_done[i], 1); }
-    for (int i = 0; i < INFO; ++i) mbar_init(&sync.info_full[i], EXPANDERS);
+    for (int i = 0; i < 2; ++i) { mbar_init(&sync.s_full[i], 1); mbar_init(&sync.p_full[i], ROW_WARPS / 2); mbar_init(&sync.pv_done[i], 1); }
+    for (int i = 0; i < INFO; ++i) mbar_init(&sync.info_full[i], UG);
+    mbar_init(&sync.x_full, ROW_WARPS);
+    mbar_init(&sync.x_empty, ROW_WARPS);
     mbar_init(&sync.drain, 1);
     sync.error = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -162,12 +223,30 @@ __global__ void __launch_bounds__(THREADS, 1) kv4_attn_tc_kernel(const Kv4Attn A
   bool ok = true;
 
   if (warp >= ROW_WARPS && warp < MMA_WARP) {
-    // ------------------------------------------------------------------ expanding warps: granule gq of every tile, K or V
-    const int w = warp - ROW_WARPS, gq = w & 3, g = lane >> 2, t = lane & 3;
-    const bool is_v = w >= 4;
+    // ------------------------------------------------------------------ expanding warps
+    const int w = warp - ROW_WARPS, g = lane >> 2, t = lane & 3;
     const uint32_t codes = sb + LY::CODES + (uint32_t)(w * RING * LY::PART);
-    uint64_t *full = is_v ? sync.v_full : sync.k_full, *empty = is_v ? sync.v_empty : sync.k_empty;
-    const uint32_t out0 = sb + (is_v ? LY::V : LY::K);
+    // where this lane's words go, by slot & 7 (K: g; V: 2t and 2t + 1), in an order in which a quarter of the warp writes to eight
+    // places of 16 bytes in different banks
+    const bool far = t >= 2, odd = (g & 1) != 0;
+    uint32_t k_at[DH / 32], v_at[2][DH / 64];
+#pragma unroll
+    for (int j = 0; j < DH / 32; ++j) {
+      const int l = DH == 128 ? 4 * t + (j ^ (far ? 2 : 0)) : 2 * t + j;
+      k_at[j] = sb + LY::K + (uint32_t)((l >> 3) * BLK + g * 128 + (((l & 7) ^ g) << 4));
+    }
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int j = 0; j < DH / 64; ++j) {
+        const int l = DH == 128 ? 2 * g + (j ^ (odd ? 1 : 0)) : g, slot = 2 * t + s;
+        v_at[s][j] = sb + LY::V + (uint32_t)((l >> 3) * BLK + slot * 128 + (((l & 7) ^ slot) << 4));
+      }
+    // the parameters: lanes 0 .. 15 K of slot `lane`, lanes 16 .. 31 V
+    const int ps = lane & 15;
+    const bool pv = lane >= 16;
+    const uint32_t p_from = (uint32_t)(KV4_G * DH + (ps & 7) * 16 + (pv ? 8 : 0) + (ps >> 3) * 4);
+    const uint32_t p_to = sb + (uint32_t)((pv ? LY::V : LY::K) + (LY::NBLK - 1) * BLK + ps * 128 + ((ps & 7) << 4));
     while (more && ok && walk.next(A, G, lane, pc)) {
       const int n = pc.hi - pc.lo, kv = min(pc.kv, pc.hi * TK), cache_row = A.rows.cache_of(pc.b);
       uint64_t or0 = ~0ull, or1 = ~0ull;   // slots behind ctx that some row sees
@@ -184,144 +263,121 @@ __global__ void __launch_bounds__(THREADS, 1) kv4_attn_tc_kernel(const Kv4Attn A
           or1 |= __shfl_xor_sync(0xffffffffu, or1, o);
         }
       }
-      auto pages_from = [&](int i) {       // of tiles i .. i + 31 of the piece
-        const int gi = (pc.lo + i + lane) * UG + gq;
-        if (i + lane >= n || gi * KV4_G >= kv) return -1;
+      const int steps = n * UG > w ? (n * UG - w + EXPANDERS - 1) / EXPANDERS : 0;      // granules w, w + EXPANDERS ..
+      auto pages_from = [&](int step) {    // of steps step .. step + 31
+        const int gi = pc.lo * UG + w + EXPANDERS * (step + lane);
+        if (step + lane >= steps || gi * KV4_G >= kv) return -1;
         const int page = A.c.page_of(cache_row, gi);
         if ((unsigned)page >= (unsigned)A.c.n_pages) A.rows.report();
         return page;
       };
       int page_now = pages_from(0), page_next = pages_from(32);
       unsigned have = 0u;
-      auto request = [&](int i) {
+      auto request = [&](int step) {
         bool there = false;
-        if (i < n) {
-          const int page = __shfl_sync(0xffffffffu, page_now, i & 31);
+        if (step < steps) {
+          const int page = __shfl_sync(0xffffffffu, page_now, step & 31);
           there = (unsigned)page < (unsigned)A.c.n_pages;
           if (there) {
-            const unsigned char *src = A.c.pages + A.layer_off + A.c.granule<DH>(page, pc.hk, (pc.lo + i) * UG + gq);
-            const uint32_t dst = codes + (uint32_t)(i % RING * LY::PART);
+            const unsigned char *src = A.c.pages + A.layer_off + A.c.granule<DH>(page, pc.hk, pc.lo * UG + w + EXPANDERS * step) + lane * 16;
+            const uint32_t dst = codes + (uint32_t)(step % RING * LY::PART + lane * 16);
 #pragma unroll
-            for (int k = 0; k < DH / 64; ++k) copy16(dst + k * 512 + lane * 16, src + (is_v ? KV4_G * DH / 2 : 0) + k * 512 + lane * 16);
-            if (lane < KV4_PARAMS / 16) copy16(dst + KV4_G * DH / 2 + lane * 16, src + KV4_G * DH + lane * 16);
+            for (int k = 0; k < LY::PART / 512; ++k) copy16(dst + k * 512, src + k * 512);
+            if (lane < (LY::PART % 512) / 16) copy16(dst + LY::PART / 512 * 512, src + LY::PART / 512 * 512);
           }
-          if ((i & 31) == 31) {
+          if ((step & 31) == 31) {
             page_now = page_next;
-            page_next = pages_from(i + 33);
+            page_next = pages_from(step + 33);
           }
         }
         have = have << 1 | (there ? 1u : 0u);
         asm volatile("cp.async.commit_group;" ::: "memory");
       };
 #pragma unroll
-      for (int i = 0; i < RING - 1; ++i) request(i);
+      for (int s = 0; s < RING - 1; ++s) request(s);
 #pragma unroll 1
-      for (int i = 0; i < n; ++i) {
+      for (int step = 0; step < steps; ++step) {
         __syncwarp();
-        request(i + RING - 1);
+        request(step + RING - 1);
         asm volatile("cp.async.wait_group %0;" ::"n"(RING - 1) : "memory");
         __syncwarp();
         const bool there = (have >> (RING - 1) & 1u) != 0u;
-        const uint32_t at = codes + (uint32_t)(i % RING * LY::PART);
-        // ---- parameters of this lane's vectors: K of slots g, g + 8; V of slots 2t, 2t + 1, 2t + 8, 2t + 9
-        constexpr int NV = 4;
-        float sc[NV], zc[NV];
-        int slot[NV];
-        {
-          const uint4 e0 = lds128(at + KV4_G * DH / 2 + (is_v ? 2 * t : g) * 16), e1 = lds128(at + KV4_G * DH / 2 + (is_v ? 2 * t + 1 : g) * 16);
-          const uint32_t p[NV] = {is_v ? e0.z : e0.x, is_v ? e1.z : e0.y, is_v ? e0.w : e0.x, is_v ? e1.w : e0.y};
+        const int unit = w + EXPANDERS * step, gq = unit & (UG - 1), now = tt + unit / UG;
+        const uint32_t at = codes + (uint32_t)(step % RING * LY::PART), buf = (uint32_t)(now % NB * LY::ONE + gq * KV4_G * 128);
+        // ---- the parameters of this lane's vector, and the granule's power of two
+        uint32_t par;
+        asm volatile("ld.shared.b32 %0, [%1];" : "=r"(par) : "r"(at + p_from) : "memory");
+        float sc = __uint_as_float(par << 16), zc = fmaf(8.f, sc, __uint_as_float(par & 0xffff0000u));
+        const int key = (pc.lo * UG + unit) * KV4_G + ps, rel = key - pc.ctx;
+        bool v = there && key < kv;
+        if (tree && rel >= 0) v = v && (rel < 64 ? (or0 >> rel) & 1ull : rel < 128 ? (or1 >> (rel - 64)) & 1ull : 0ull) != 0ull;
+        const bool finite = fabsf(zc) < INFINITY && sc < INFINITY;
+        const unsigned poison = __ballot_sync(0xffffffffu, v && !finite);
+        if (!v || !finite) { sc = 0.f; zc = 0.f; }
+        float most = fmaxf(8.f * sc, fabsf(zc));
 #pragma unroll
-          for (int k = 0; k < NV; ++k) {
-            slot[k] = is_v ? 2 * t + (k & 1) + 8 * (k >> 1) : g + 8 * (k & 1);
-            sc[k] = __uint_as_float(p[k] << 16);
-            zc[k] = fmaf(8.f, sc[k], __uint_as_float(p[k] & 0xffff0000u));
-          }
-        }
-        const int key0 = (pc.lo + i) * TK + gq * KV4_G;
-        float most = 0.f;
-        unsigned poison = 0u;              // this lane's slots
-#pragma unroll
-        for (int k = 0; k < NV; ++k) {
-          const int key = key0 + slot[k], rel = key - pc.ctx;
-          bool v = there && key < kv;
-          if (tree && rel >= 0) v = v && (rel < 64 ? (or0 >> rel) & 1ull : rel < 128 ? (or1 >> (rel - 64)) & 1ull : 0ull) != 0ull;
-          const bool finite = fabsf(zc[k]) < INFINITY && sc[k] < INFINITY;
-          if (v && !finite) poison |= 1u << slot[k];
-          if (!v || !finite) { sc[k] = 0.f; zc[k] = 0.f; }
-          most = fmaxf(most, fmaxf(8.f * sc[k], fabsf(zc[k])));
-        }
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
-        if (__any_sync(0xffffffffu, poison != 0u)) {
-#pragma unroll
-          for (int o = 1; o < 32; o <<= 1) poison |= __shfl_xor_sync(0xffffffffu, poison, o);
-        }
+        for (int o = 1; o < 16; o <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
         const int ex = most > 0.f ? max(-112, (int)(__float_as_uint(most) >> 23) - 127) : 13;      // most in [2^ex, 2^(ex + 1))
         const float norm = pow2i(13 - ex);
-        const int now = tt + i;
-        if (lane == 0) {
+        if (ps == 0) {
           TileInfo &f = sync.info[now & (INFO - 1)];
-          if (is_v) {
+          if (pv) {
             f.v_exp[gq] = most > 0.f ? ex - 13 : -200;
-            f.poison_v[gq] = poison;
+            f.poison_v[gq] = poison >> 16;
           } else {
-            f.k_back[gq] = 1.f / norm;
-            f.poison[gq] = poison;
+            f.k_back[gq] = pow2i(ex - 13);
+            f.poison[gq] = poison & 0xffffu;
           }
-          arrive(&sync.info_full[now & (INFO - 1)]);
         }
-        if (now >= NB) ok = __all_sync(0xffffffffu, mbar_wait(&empty[now % NB], (uint32_t)(now / NB - 1) & 1u));
-        if (!ok) break;
-        const uint32_t out = out0 + (uint32_t)(now % NB * LY::ONE);
-        auto put = [&](uint32_t word, int s, int l, float scale) {
-          const int key = gq * KV4_G + s;
-          const __half2 sc2 = __float2half2_rn(scale * norm);
-          uint32_t x[4];
-          expand(word, sc2, x);
-          sts128(out + (uint32_t)((l >> 3) * BLK + key * 128 + (((l & 7) ^ (key & 7)) << 4)), x[0], x[1], x[2], x[3]);
-        };
+        __syncwarp();
+        if (lane == 0) arrive(&sync.info_full[now & (INFO - 1)]);
+        const float z = zc * norm, zh = __half2float(__float2half_rn(z));
+        const uint32_t consts = pack2(zh, z - zh), scale2 = pack2(sc * norm, sc * norm);
+        // ---- K
         const uint4 c0 = lds128(at + lane * 16), c1 = DH == 128 ? lds128(at + 512 + lane * 16) : c0;
+        const __half2 ka = as_half2(__shfl_sync(0xffffffffu, scale2, g)), kb = as_half2(__shfl_sync(0xffffffffu, scale2, g + 8));
+        if (now >= NB) ok = __all_sync(0xffffffffu, mbar_wait(&sync.k_empty[now % NB], (uint32_t)(now / NB - 1) & 1u));
+        if (!ok) break;
+        auto put = [&](uint32_t word, __half2 s2, uint32_t to) {
+          uint32_t x[4];
+          expand(word, s2, x);
+          sts128(to, x[0], x[1], x[2], x[3]);
+        };
         if constexpr (DH == 128) {
-          // words in an order in which a quarter of the warp writes to eight places of 16 bytes that lie in different banks
-          if (is_v) {
-            const bool odd = (g & 1) != 0;
-            const int l0 = 2 * g + (odd ? 1 : 0), l1 = 2 * g + (odd ? 0 : 1);
-            put(odd ? c0.y : c0.x, slot[0], l0, sc[0]); put(odd ? c0.x : c0.y, slot[0], l1, sc[0]);
-            put(odd ? c0.w : c0.z, slot[1], l0, sc[1]); put(odd ? c0.z : c0.w, slot[1], l1, sc[1]);
-            put(odd ? c1.y : c1.x, slot[2], l0, sc[2]); put(odd ? c1.x : c1.y, slot[2], l1, sc[2]);
-            put(odd ? c1.w : c1.z, slot[3], l0, sc[3]); put(odd ? c1.z : c1.w, slot[3], l1, sc[3]);
-          } else {
-            const bool far = t >= 2;
-            const int f2 = far ? 2 : 0;
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-              const uint4 c = k == 0 ? c0 : c1;
-              put(far ? c.z : c.x, slot[k], 4 * t + (0 ^ f2), sc[k]);
-              put(far ? c.w : c.y, slot[k], 4 * t + (1 ^ f2), sc[k]);
-              put(far ? c.x : c.z, slot[k], 4 * t + (2 ^ f2), sc[k]);
-              put(far ? c.y : c.w, slot[k], 4 * t + (3 ^ f2), sc[k]);
-            }
-          }
-        } else if (is_v) {
-          put(c0.x, slot[0], g, sc[0]); put(c0.y, slot[1], g, sc[1]); put(c0.z, slot[2], g, sc[2]); put(c0.w, slot[3], g, sc[3]);
+          put(far ? c0.z : c0.x, ka, k_at[0] + buf); put(far ? c0.w : c0.y, ka, k_at[1] + buf);
+          put(far ? c0.x : c0.z, ka, k_at[DH / 32 - 2] + buf); put(far ? c0.y : c0.w, ka, k_at[DH / 32 - 1] + buf);
+          put(far ? c1.z : c1.x, kb, k_at[0] + buf + 1024); put(far ? c1.w : c1.y, kb, k_at[1] + buf + 1024);
+          put(far ? c1.x : c1.z, kb, k_at[DH / 32 - 2] + buf + 1024); put(far ? c1.y : c1.w, kb, k_at[DH / 32 - 1] + buf + 1024);
         } else {
-          put(c0.x, slot[0], 2 * t, sc[0]); put(c0.y, slot[0], 2 * t + 1, sc[0]);
-          put(c0.z, slot[1], 2 * t, sc[1]); put(c0.w, slot[1], 2 * t + 1, sc[1]);
+          put(c0.x, ka, k_at[0] + buf); put(c0.y, ka, k_at[1] + buf);
+          put(c0.z, kb, k_at[0] + buf + 1024); put(c0.w, kb, k_at[1] + buf + 1024);
         }
-        // ---- the constants: K has them twice side by side (for the two values of Z), V once
-        if (is_v ? g == 0 : t == 0) {
-#pragma unroll
-          for (int k = 0; k < NV; ++k) {
-            if (!is_v && k >= 2) break;
-            const int key = gq * KV4_G + slot[k];
-            const float z = zc[k] * norm, zh = __half2float(__float2half_rn(z));
-            const uint32_t both = pack2(zh, z - zh);
-            sts128(out + (uint32_t)((LY::NBLK - 1) * BLK + key * 128 + ((key & 7) << 4)), both, is_v ? 0u : both, 0u, 0u);
-          }
-        }
+        // the constants: K has them twice side by side (for the two values of Z), V once
+        if (!pv) sts128(p_to + buf, consts, consts, 0u, 0u);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
-        if (lane == 0) arrive(&full[now % NB]);
+        if (lane == 0) arrive(&sync.k_full[now % NB]);
+        // ---- V
+        const uint32_t vat = at + KV4_G * DH / 2 + lane * 16;
+        const uint4 d0 = lds128(vat), d1 = DH == 128 ? lds128(vat + 512) : d0;
+        __half2 vs[4];
+#pragma unroll
+        for (int s = 0; s < 4; ++s) vs[s] = as_half2(__shfl_sync(0xffffffffu, scale2, 16 + 2 * t + (s & 1) + 8 * (s >> 1)));
+        if (now >= NB) ok = __all_sync(0xffffffffu, mbar_wait(&sync.v_empty[now % NB], (uint32_t)(now / NB - 1) & 1u));
+        if (!ok) break;
+        if constexpr (DH == 128) {
+          put(odd ? d0.y : d0.x, vs[0], v_at[0][0] + buf); put(odd ? d0.x : d0.y, vs[0], v_at[0][DH / 64 - 1] + buf);
+          put(odd ? d0.w : d0.z, vs[1], v_at[1][0] + buf); put(odd ? d0.z : d0.w, vs[1], v_at[1][DH / 64 - 1] + buf);
+          put(odd ? d1.y : d1.x, vs[2], v_at[0][0] + buf + 1024); put(odd ? d1.x : d1.y, vs[2], v_at[0][DH / 64 - 1] + buf + 1024);
+          put(odd ? d1.w : d1.z, vs[3], v_at[1][0] + buf + 1024); put(odd ? d1.z : d1.w, vs[3], v_at[1][DH / 64 - 1] + buf + 1024);
+        } else {
+          put(d0.x, vs[0], v_at[0][0] + buf); put(d0.y, vs[1], v_at[1][0] + buf);
+          put(d0.z, vs[2], v_at[0][0] + buf + 1024); put(d0.w, vs[3], v_at[1][0] + buf + 1024);
+        }
+        if (pv) sts128(p_to + buf, consts, 0u, 0u, 0u);
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) arrive(&sync.v_full[now % NB]);
       }
       asm volatile("cp.async.wait_group 0;" ::: "memory");
       tt += n;
@@ -331,50 +387,53 @@ __global__ void __launch_bounds__(THREADS, 1) kv4_attn_tc_kernel(const Kv4Attn A
     // ------------------------------------------------------------------ MMA issuer
     const uint32_t idesc_s = (1u << 4) | ((uint32_t)(TK >> 3) << 17) | ((128u >> 4) << 24);                                  // fp32, fp16 x fp16, N = 64
     const uint32_t idesc_o = (1u << 4) | (1u << 16) | ((uint32_t)((DH + 16) >> 3) << 17) | ((128u >> 4) << 24);               // N = DH + 16, B MN-major
+    const uint32_t leader = lane == 0 ? 1u : 0u;
     int pieces = 0;
     while (more && ok && walk.next(A, G, lane, pc)) {
       const int n = pc.hi - pc.lo;
-      if (n > 0 && lane == 0) {
+      if (n > 0) {
         auto issue_s = [&](int now) -> bool {
-          if (!mbar_wait(&sync.k_full[now % NB], (uint32_t)(now / NB) & 1u)) return false;
+          if (!__all_sync(0xffffffffu, mbar_wait(&sync.k_full[now % NB], (uint32_t)(now / NB) & 1u))) return false;
           fence_after();
-          const uint32_t kb = sb + LY::K + (uint32_t)(now % NB * LY::ONE), d = tmem + (uint32_t)(COL_S + (now & 1) * TK);
+          const uint64_t kb = smem_desc_sw128(sb + LY::K + (uint32_t)(now % NB * LY::ONE));
+          const uint32_t d = tmem + (uint32_t)(COL_S + (now & 1) * TK);
 #pragma unroll
           for (int k = 0; k < DH / 16 + 1; ++k)             // the last step: the constants
-            umma_ts(d, tmem + (uint32_t)(COL_Q + 8 * k), smem_desc_sw128(kb + (uint32_t)((k >> 2) * BLK)) + (uint64_t)(2 * (k & 3)), idesc_s, k ? 1u : 0u);
-          umma_commit(&sync.s_full[now & 1]);
-          umma_commit(&sync.k_empty[now % NB]);
+            umma_ts(leader, d, tmem + (uint32_t)(COL_Q + 8 * k), kb + (uint64_t)(((k >> 2) * BLK >> 4) + 2 * (k & 3)), idesc_s, k ? 1u : 0u);
+          commit(leader, &sync.s_full[now & 1]);
+          commit(leader, &sync.k_empty[now % NB]);
           return true;
         };
         auto issue_pv = [&](int now, bool first) -> bool {
-          if (!mbar_wait(&sync.p_full[now & 1], (uint32_t)(now >> 1) & 1u)) return false;
-          if (!mbar_wait(&sync.v_full[now % NB], (uint32_t)(now / NB) & 1u)) return false;
+          if (!__all_sync(0xffffffffu, mbar_wait(&sync.p_full[now & 1], (uint32_t)(now >> 1) & 1u))) return false;
+          if (!__all_sync(0xffffffffu, mbar_wait(&sync.v_full[now % NB], (uint32_t)(now / NB) & 1u))) return false;
           fence_after();
-          const uint32_t vb = sb + LY::V + (uint32_t)(now % NB * LY::ONE), p = tmem + (uint32_t)(COL_S + (now & 1) * TK);
+          const uint64_t vb = smem_desc_mn_sw128(sb + LY::V + (uint32_t)(now % NB * LY::ONE), BLK, 1024);
+          const uint32_t p = tmem + (uint32_t)(COL_S + (now & 1) * TK), d = tmem + (uint32_t)(COL_O + (now & 1) * O_COLS);
 #pragma unroll
-          for (int k = 0; k < TK / 16; ++k)
-            umma_ts(tmem + (uint32_t)COL_O, p + (uint32_t)(8 * k), smem_desc_mn_sw128(vb + (uint32_t)(k * 2048), BLK, 1024), idesc_o, (first && k == 0) ? 0u : 1u);
-          umma_commit(&sync.v_empty[now % NB]);
-          umma_commit(&sync.pv_done[now & 1]);
+          for (int k = 0; k < TK / 16; ++k) umma_ts(leader, d, p + (uint32_t)(8 * k), vb + (uint64_t)(k * 2048 >> 4), idesc_o, (first && k == 0) ? 0u : 1u);
+          commit(leader, &sync.v_empty[now % NB]);
+          commit(leader, &sync.pv_done[now & 1]);
           return true;
         };
-        ok = mbar_wait(&sync.q_full, (uint32_t)pieces & 1u);
+        ok = __all_sync(0xffffffffu, mbar_wait(&sync.q_full, (uint32_t)pieces & 1u));
         for (int i = -1; i < n && ok; ++i) {
           if (i + 1 < n) ok = issue_s(tt + i + 1);
-          if (i >= 0 && ok) ok = issue_pv(tt + i, i == 0);
+          if (i >= 0 && ok) ok = issue_pv(tt + i, i < 2);          // the first of either group
         }
       }
-      ok = __all_sync(0xffffffffu, ok);
       if (n > 0) ++pieces;
       tt += n;
     }
     if (!ok) atomicExch(&sync.error, 1);
-  } else if (warp < ROW_WARPS) {
+  } else {
     // ------------------------------------------------------------------ rows
+    const int quarter = warp & 3, group = warp >> 2;      // tensor-memory lanes 32 quarter ..; tiles with now % 2 == group
     const int half = MODE == FULL ? 0 : lane >> 4;
-    const int row = MODE == FULL ? warp * 32 + lane : warp * 16 + (lane & 15);
-    const uint32_t lanes = (uint32_t)(warp * 32) << 16;
+    const int row = MODE == FULL ? quarter * 32 + lane : quarter * 16 + (lane & 15);
+    const uint32_t mine = tmem + ((uint32_t)(quarter * 32) << 16), o_at = mine + (uint32_t)(COL_O + group * O_COLS);
     const float log2_scale = A.scale * 1.4426950408889634f;
+    int pieces = 0;
     while (more && ok && walk.next(A, G, lane, pc)) {
       const int n = pc.hi - pc.lo, kv = min(pc.kv, pc.hi * TK);
       const int rr = pc.row0 + row, n_rows = pc.count * G, i_row = A.by_group(rr);
@@ -383,77 +442,102 @@ __global__ void __launch_bounds__(THREADS, 1) kv4_attn_tc_kernel(const Kv4Attn A
       int k_ref = -200;
       bool nan_row = false, have_o = false;
       if (n > 0) {
-        // ---- Q into tensor memory: column d holds dims d and d + DH/2
-        const long long at = in ? (long long)(pc.first + i_row) * A.q.row + (long long)(pc.hk * G + rr - i_row * G) * A.q.head : 0;
-        auto four = [&](int d, float *x) {
-          if (!in) { x[0] = x[1] = x[2] = x[3] = 0.f; return; }
+        // ---- Q into tensor memory: column d holds dims d and d + DH/2; group 0 writes the first half of the columns.  (Short code: it runs
+        // once a piece, and fetching it is most of what it takes)
+        // The rows come through shared memory, a warp reading whole rows (read by the threads that own them, every load would touch
+        // 32 lines): eight bytes at a time, piece c of row r at place c ^ (r & 15) (c ^ 2 (r & 7), pairs of places, for fp32).
+        constexpr int ROW_B = DH * (MODE == PAIR ? 4 : 2), PER = ROW_B / 8, WARP_ROWS = ROWS / 4;
+        const uint32_t q_rows = sb + LY::Q + (uint32_t)(quarter * WARP_ROWS * ROW_B);
+#pragma unroll 4
+        for (int e = lane; e < WARP_ROWS / 2 * PER; e += 32) {
+          const int r = group * (WARP_ROWS / 2) + e / PER, c = e % PER, rq = pc.row0 + quarter * WARP_ROWS + r;
+          if (rq >= n_rows) continue;
+          const int iq = A.by_group(rq);
+          const unsigned char *src = reinterpret_cast<const unsigned char *>(A.q.p) +
+                                     ((long long)(pc.first + iq) * A.q.row + (long long)(pc.hk * G + rq - iq * G) * A.q.head) * (MODE == PAIR ? 4 : 2) + c * 8;
+          copy8(q_rows + (uint32_t)(r * ROW_B + (c ^ (MODE == PAIR ? 2 * (r & 7) : r & 15)) * 8), src);
+        }
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) arrive(&sync.q_in);
+        ok = __all_sync(0xffffffffu, mbar_wait(&sync.q_in, (uint32_t)pieces & 1u));
+        if (!ok) break;
+        float top = 0.f, sum = 0.f;
+        constexpr int QC = DH / 4;         // columns of a group
+        const bool is_bf16 = A.q_type == KV4_BF16;
+        const int r_in = MODE == FULL ? lane : lane & 15;
+        const uint32_t my_row = q_rows + (uint32_t)(r_in * ROW_B);
+        auto four = [&](int d) -> float4 {
+          if (!in) return make_float4(0.f, 0.f, 0.f, 0.f);
           if constexpr (MODE == PAIR) {
-            const float4 v = *reinterpret_cast<const float4 *>(reinterpret_cast<const float *>(A.q.p) + at + d);
-            x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
+            const uint4 v = lds128(my_row + (uint32_t)(((d / 2) ^ (2 * (r_in & 7))) * 8));
+            return make_float4(__uint_as_float(v.x), __uint_as_float(v.y), __uint_as_float(v.z), __uint_as_float(v.w));
           } else {
-            const uint2 v = *reinterpret_cast<const uint2 *>(reinterpret_cast<const __half *>(A.q.p) + at + d);
-            const bool is_bf16 = A.q_type == KV4_BF16;
-            const float2 a = is_bf16 ? make_float2(__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xffff0000u)) : unpack2(v.x);
-            const float2 b = is_bf16 ? make_float2(__uint_as_float(v.y << 16), __uint_as_float(v.y & 0xffff0000u)) : unpack2(v.y);
-            x[0] = a.x; x[1] = a.y; x[2] = b.x; x[3] = b.y;
+            const uint2 v = lds64(my_row + (uint32_t)(((d / 4) ^ (r_in & 15)) * 8));
+            const float2 a = unpack2(v.x), b = unpack2(v.y);
+            return is_bf16 ? make_float4(__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xffff0000u), __uint_as_float(v.y << 16), __uint_as_float(v.y & 0xffff0000u))
+                           : make_float4(a.x, a.y, b.x, b.y);
           }
         };
-        float top = 0.f, sum = 0.f;
-#pragma unroll 8
-        for (int d = 0; d < DH; d += 4) {
-          float x[4];
-          four(d, x);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) { top = fmaxf(top, fabsf(x[e])); sum += x[e]; }
-        }
-        const int ex = max(-112, min((int)(__float_as_uint(top) >> 23) - 127, 126));
-        const float up = pow2i(7 - ex);
-        factor_row = fminf(log2_scale / up, 3e38f);
 #pragma unroll 1
-        for (int c = 0; c < DH / 2; c += 16) {
-          uint32_t q[16];
+        for (int d = 0; d < DH; d += 32) {
+          float4 x[8];
 #pragma unroll
-          for (int e = 0; e < 16; e += 4) {
-            float x[4], y[4];
-            four(c + e, x);
-            four(DH / 2 + c + e, y);
+          for (int k = 0; k < 8; ++k) x[k] = four(d + 4 * k);
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            top = fmaxf(max3(top, fabsf(x[k].x), fabsf(x[k].y)), fmaxf(fabsf(x[k].z), fabsf(x[k].w)));
+            sum += (x[k].x + x[k].y) + (x[k].z + x[k].w);
+          }
+        }
+        const float up = pow2i(7 - max(-112, min((int)(__float_as_uint(top) >> 23) - 127, 126)));
+#pragma unroll 1
+        for (int c = 0; c < QC; c += 16) {
+          uint32_t q[16];
+          const int d0 = group * QC + c;
+#pragma unroll
+          for (int d = 0; d < 16; d += 4) {
+            const float4 v = four(d0 + d), u = four(DH / 2 + d0 + d);
+            const float a[4] = {v.x * up, v.y * up, v.z * up, v.w * up}, b[4] = {u.x * up, u.y * up, u.z * up, u.w * up};
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-              const float a = x[k] * up, b = y[k] * up;
-              q[e + k] = pack2(a, b);
+              q[d + k] = pack2(a[k], b[k]);
               if constexpr (MODE == PAIR) {
-                const float2 h = unpack2(q[e + k]);
-                if (half) q[e + k] = pack2(a - h.x, b - h.y);
+                const float2 h = unpack2(q[d + k]);
+                if (half) q[d + k] = pack2(a[k] - h.x, b[k] - h.y);
               }
             }
           }
           __syncwarp();
-          tmem_st16(tmem + lanes + (uint32_t)(COL_Q + c), q);
+          tmem_st16(mine + (uint32_t)(COL_Q + d0), q);
         }
-        {
+        factor_row = fminf(log2_scale / up, 3e38f);
+        if (group == 1) {
           // the row's sum against the constants, as two values (three with two parts: the second lane adds the rest)
           const float z = sum * up, zh = __half2float(__float2half_rn(z)), zl = __half2float(__float2half_rn(z - zh)), zr = z - zh - zl;
-          uint32_t q[8] = {pack2(zh, zh), pack2(zl, zl), 0u, 0u, 0u, 0u, 0u, 0u};
-          if (MODE == PAIR && half) { q[0] = pack2(zr, zr); q[1] = 0u; }
-          asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(tmem + lanes + (uint32_t)(COL_Q + DH / 2)),
-                       "r"(q[0]), "r"(q[1]), "r"(q[2]), "r"(q[3]), "r"(q[4]), "r"(q[5]), "r"(q[6]), "r"(q[7]) : "memory");
+          uint32_t c[2] = {pack2(zh, zh), pack2(zl, zl)};
+          if (MODE == PAIR && half) { c[0] = pack2(zr, zr); c[1] = 0u; }
+          asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %3, %3, %3, %3, %3};" ::"r"(mine + (uint32_t)(COL_Q + DH / 2)),
+                       "r"(c[0]), "r"(c[1]), "r"(0u) : "memory");
         }
         wait_st();
         fence_before();
         __syncwarp();
         if (lane == 0) arrive(&sync.q_full);
+        // both groups have read both O of the piece before, and the sums
+        if (pieces > 0) ok = __all_sync(0xffffffffu, mbar_wait(&sync.x_empty, (uint32_t)(pieces - 1) & 1u));
       }
       const bool used = in && !(A.rows.slot != nullptr && A.rows.slot[pc.first + i_row] < 0);
       const uint64_t mk0 = tree && used ? A.rows.mask[(size_t)(pc.first + i_row) * 2] : 0ull, mk1 = tree && used ? A.rows.mask[(size_t)(pc.first + i_row) * 2 + 1] : 0ull;
       const int sees_below = !used ? 0 : tree ? kv : min(kv, pc.ctx + i_row + 1);
 #pragma unroll 1
-      for (int i = 0; i < n; ++i) {
+      for (int i = (tt & 1) == group ? 0 : 1; i < n && ok; i += 2) {
         const int now = tt + i;
-        ok = __all_sync(0xffffffffu, mbar_wait(&sync.info_full[now & (INFO - 1)], (uint32_t)(now / INFO) & 1u) && mbar_wait(&sync.s_full[now & 1], (uint32_t)(now >> 1) & 1u));
+        ok = __all_sync(0xffffffffu, mbar_wait(&sync.info_full[now & (INFO - 1)], (uint32_t)(now / INFO) & 1u) && mbar_wait(&sync.s_full[group], (uint32_t)(now >> 1) & 1u));
         if (!ok) break;
         fence_after();
         const TileInfo &f = sync.info[now & (INFO - 1)];
-        const uint32_t s_at = tmem + lanes + (uint32_t)(COL_S + (now & 1) * TK);
+        const uint32_t s_at = mine + (uint32_t)(COL_S + group * TK);
         float v[NC];
         {
           uint32_t all[TK];
@@ -489,16 +573,17 @@ __global__ void __launch_bounds__(THREADS, 1) kv4_attn_tc_kernel(const Kv4Attn A
 #pragma unroll
             for (int k = 0; k < UG; ++k) nan_row = nan_row || (see >> (KV4_G * k) & (f.poison[k] | f.poison_v[k])) != 0ull;
           }
-          see >>= NC * half;
+          const uint32_t see0 = (uint32_t)(see >> (32 * half)), see1 = (uint32_t)(see >> 32);
 #pragma unroll
-          for (int j = 0; j < NC; ++j) v[j] = (see >> j & 1ull) ? v[j] : -INFINITY;
+          for (int j = 0; j < NC; ++j) v[j] = ((j < 32 ? see0 : see1) >> (j & 31) & 1u) ? v[j] : -INFINITY;
         }
         float m_t = -INFINITY;
 #pragma unroll
         for (int k = 0; k < NG; ++k) {
-          float a = v[16 * k], b = v[16 * k + 1];
-#pragma unroll
-          for (int j = 2; j < 16; j += 2) { a = fmaxf(a, v[16 * k + j]); b = fmaxf(b, v[16 * k + j + 1]); }
+          float a = max3(v[16 * k], v[16 * k + 1], v[16 * k + 2]), b = max3(v[16 * k + 3], v[16 * k + 4], v[16 * k + 5]);
+          a = max3(a, v[16 * k + 6], v[16 * k + 7]); b = max3(b, v[16 * k + 8], v[16 * k + 9]);
+          a = max3(a, v[16 * k + 10], v[16 * k + 11]); b = max3(b, v[16 * k + 12], v[16 * k + 13]);
+          a = max3(a, v[16 * k + 14], v[16 * k + 15]);
           m_t = fmaxf(m_t, fmaxf(a, b) * fk[k]);
         }
         if (MODE != FULL) m_t = fmaxf(m_t, __shfl_xor_sync(0xffffffffu, m_t, 16));
@@ -509,64 +594,68 @@ __global__ void __launch_bounds__(THREADS, 1) kv4_attn_tc_kernel(const Kv4Attn A
         }
         const int k_was = k_ref;
         k_ref = max(k_ref, top_exp);
-        const bool rescale = have_o && (k_ref != k_was || __any_sync(0xffffffffu, factor != 1.f));
+        const bool change = __any_sync(0xffffffffu, factor != 1.f) || k_ref != k_was;
         l_run *= factor;
-        if (rescale) {
-          // every P V issued so far has landed before O is touched; none is issued before this warp has handed over its P
-          ok = __all_sync(0xffffffffu, mbar_wait(&sync.pv_done[(now - 1) & 1], (uint32_t)((now - 1) >> 1) & 1u));
+        if (have_o && change) {
+          // the P V of this group's tile before has landed before O is touched; none is issued before this warp has handed over its P
+          ok = __all_sync(0xffffffffu, mbar_wait(&sync.pv_done[group], (uint32_t)((now - 2) >> 1) & 1u));
           if (!ok) break;
           fence_after();
-          const float both = factor * (k_was - k_ref < -126 ? 0.f : pow2i(k_was - k_ref));
+          const float scaled = factor * (k_was - k_ref < -126 ? 0.f : pow2i(k_was - k_ref));
 #pragma unroll 1
           for (int c = 0; c < DH + 16; c += 16) {
             uint32_t o[16];
-            tmem_ld16(tmem + lanes + (uint32_t)(COL_O + c), o);
+            tmem_ld16(o_at + (uint32_t)c, o);
             wait_ld();
 #pragma unroll
-            for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * both);
-            tmem_st16(tmem + lanes + (uint32_t)(COL_O + c), o);
+            for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * scaled);
+            tmem_st16(o_at + (uint32_t)c, o);
           }
           wait_st();
         }
         const float mu = m_run == -INFINITY ? 0.f : m_run;
+        const f32x2 mu2 = both(-mu, -mu);
         uint32_t p[NC / 2], p_lo[MODE == PAIR ? NC / 2 : 1];
-        float l4[4] = {0.f, 0.f, 0.f, 0.f};
+        f32x2 l2[2] = {both(l_run, 0.f), both(0.f, 0.f)};
 #pragma unroll
         for (int k = 0; k < NG; ++k) {
           const float pg = pow2i(max(f.v_exp[NG * half + k] - k_ref, -110) + P_TOP);
+          const f32x2 pg2 = both(pg, pg), fk2 = both(fk[k], fk[k]);
 #pragma unroll
           for (int j = 0; j < 16; j += 2) {
-            const float a = ex2(fmaf(v[16 * k + j], fk[k], -mu)), b = ex2(fmaf(v[16 * k + j + 1], fk[k], -mu));
-            l4[j & 2] += a;
-            l4[(j & 2) + 1] += b;
-            const uint32_t h = pack2(a * pg, b * pg);
+            const float2 e = apart(fma2(both(v[16 * k + j], v[16 * k + j + 1]), fk2, mu2));
+            const f32x2 ab = both(ex2(e.x), ex2(e.y));
+            l2[(j >> 1) & 1] = add2(l2[(j >> 1) & 1], ab);
+            const float2 w = apart(mul2(ab, pg2));
+            const uint32_t h = pack2(w.x, w.y);
             p[8 * k + j / 2] = h;
             if constexpr (MODE == PAIR) {
               const float2 back = unpack2(h);
-              p_lo[8 * k + j / 2] = pack2(a * pg - back.x, b * pg - back.y);
+              p_lo[8 * k + j / 2] = pack2(w.x - back.x, w.y - back.y);
             }
           }
         }
-        l_run += (l4[0] + l4[1]) + (l4[2] + l4[3]);
+        {
+          const float2 s = apart(add2(l2[0], l2[1]));
+          l_run = s.x + s.y;
+        }
         __syncwarp();
         // ---- P where S was: every lane of this warp has read its S
         if constexpr (MODE == FULL) {
           tmem_st16(s_at, p);
           tmem_st16(s_at + 16u, p + 16);
-        } else if constexpr (MODE == HALF) {
-          uint32_t a[16], b[16];
-#pragma unroll
-          for (int j = 0; j < 16; ++j) { a[j] = half ? 0u : p[j]; b[j] = half ? p[j] : 0u; }
-          tmem_st16(s_at, a);
-          tmem_st16(s_at + 16u, b);
         } else {
-          // lane l: the values of all keys, lane l + 16: the residuals
-          uint32_t a[16], b[16];
+          uint32_t a[16], b[16];           // keys 0 .. 31, 32 .. 63
 #pragma unroll
           for (int j = 0; j < 16; ++j) {
-            const uint32_t other = __shfl_xor_sync(0xffffffffu, half ? p[j] : p_lo[j], 16);
-            a[j] = half ? other : p[j];          // keys 0 .. 31
-            b[j] = half ? p_lo[j] : other;       // keys 32 .. 63
+            if constexpr (MODE == HALF) {
+              a[j] = half ? 0u : p[j];
+              b[j] = half ? p[j] : 0u;
+            } else {                       // lane l: the values of all keys, lane l + 16: the residuals
+              const uint32_t other = __shfl_xor_sync(0xffffffffu, half ? p[j] : p_lo[j], 16);
+              a[j] = half ? other : p[j];
+              b[j] = half ? p_lo[j] : other;
+            }
           }
           tmem_st16(s_at, a);
           tmem_st16(s_at + 16u, b);
@@ -574,14 +663,15 @@ __global__ void __launch_bounds__(THREADS, 1) kv4_attn_tc_kernel(const Kv4Attn A
         wait_st();
         fence_before();
         __syncwarp();
-        if (lane == 0) arrive(&sync.p_full[now & 1]);
+        if (lane == 0) arrive(&sync.p_full[group]);
         have_o = true;
       }
       if (!ok) break;
-      // ---- the piece's result
+      // ---- the piece's result: both groups' products have landed
       if (n > 0) {
-        const int last = tt + n - 1;
-        ok = __all_sync(0xffffffffu, mbar_wait(&sync.pv_done[last & 1], (uint32_t)(last >> 1) & 1u));
+        const int last = tt + n - 1, last_other = last - 1;
+        ok = __all_sync(0xffffffffu, mbar_wait(&sync.pv_done[last & 1], (uint32_t)(last >> 1) & 1u) &&
+                                         (n < 2 || mbar_wait(&sync.pv_done[last_other & 1], (uint32_t)(last_other >> 1) & 1u)));
         if (!ok) break;
         fence_after();
       }
@@ -591,49 +681,67 @@ __global__ void __launch_bounds__(THREADS, 1) kv4_attn_tc_kernel(const Kv4Attn A
         nan_row = nan_row || other != 0;
       }
       if (nan_row) l_run = NAN;
-      const float unit = exp2f((float)(k_ref - P_TOP));
-      float zs = 0.f;
+      // ---- the groups together: group 0 writes the first half of the dims' words, group 1 the second
+      float2 ml = make_float2(m_run, l_run);
+      float unit[2] = {0.f, 0.f};
       if (n > 0) {
-        uint32_t o[16];
-        tmem_ld16(tmem + lanes + (uint32_t)(COL_O + DH), o);
-        wait_ld();
-        zs = __uint_as_float(o[0]) + __uint_as_float(o[1]);
-        if (MODE != FULL) zs += __shfl_xor_sync(0xffffffffu, zs, 16);
+        if (half == 0) sync.x[group][row] = make_float4(m_run, l_run, have_o ? exp2f((float)(k_ref - P_TOP)) : 0.f, 0.f);
+        __syncwarp();
+        if (lane == 0) arrive(&sync.x_full);
+        ok = __all_sync(0xffffffffu, mbar_wait(&sync.x_full, (uint32_t)pieces & 1u));
+        if (!ok) break;
+        const float4 x0 = sync.x[0][row], x1 = sync.x[1][row];
+        const float top = fmaxf(x0.x, x1.x), f0 = share(make_float2(x0.x, x0.y), top), f1 = share(make_float2(x1.x, x1.y), top);
+        ml = make_float2(top, (x0.x == -INFINITY ? x0.y : f0 * x0.y) + (x1.x == -INFINITY ? x1.y : f1 * x1.y));
+        unit[0] = x0.z * f0;
+        unit[1] = x1.z * f1;
       }
+      const float inv = !pc.whole ? 1.f : ml.y != 0.f && (used || !in) ? 1.f / ml.y : 0.f;      // nothing seen, or not in use: 0
       float *part = part_of<DH, ROWS>(scratch, blockIdx.x, pc.begins) + row * PART_ROW<DH>;
+      const long long out = in ? (long long)(pc.first + i_row) * A.out.row + (long long)(pc.hk * G + rr - i_row * G) * A.out.head : 0;
+      float zs[2];
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        uint32_t o[8];
+        tmem_ld8(mine + (uint32_t)(COL_O + k * O_COLS + DH), o);
+        wait_ld();
+        zs[k] = __uint_as_float(o[0]) + __uint_as_float(o[1]);
+        if (MODE != FULL) zs[k] += __shfl_xor_sync(0xffffffffu, zs[k], 16);
+        unit[k] *= inv;
+      }
 #pragma unroll 1
-      for (int c = 0; c < DH; c += 16) {   // two words: dims 4l .. 4l + 3 and DH/2 + 4l ..
-        uint32_t o[16];
+      for (int l = group * (DH / 16); l < (group + 1) * (DH / 16); ++l) {      // words: dims 4l .. 4l + 3 and DH/2 + 4l ..
+        uint32_t o[2][8];
+        tmem_ld8(mine + (uint32_t)(COL_O + 8 * l), o[0]);
+        tmem_ld8(mine + (uint32_t)(COL_O + O_COLS + 8 * l), o[1]);
+        wait_ld();
+        float x[8];
 #pragma unroll
-        for (int j = 0; j < 16; ++j) o[j] = 0u;
-        if (n > 0) {
-          tmem_ld16(tmem + lanes + (uint32_t)(COL_O + c), o);
-          wait_ld();
+        for (int j = 0; j < 8; ++j) {
+          x[j] = 0.f;
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            float a = __uint_as_float(o[k][j]);
+            if (MODE != FULL) a += __shfl_xor_sync(0xffffffffu, a, 16);
+            if (unit[k] != 0.f) x[j] = fmaf(a + zs[k], unit[k], x[j]);         // (an O that was never written may hold anything)
+          }
         }
-        float x[16];
-#pragma unroll
-        for (int j = 0; j < 16; ++j) {
-          x[j] = __uint_as_float(o[j]);
-          if (MODE != FULL) x[j] += __shfl_xor_sync(0xffffffffu, x[j], 16);
-          x[j] = (x[j] + zs) * unit;
-        }
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          if (!in || (MODE != FULL && k != half)) continue;
-          const int d = 4 * (c / 8 + k);
-          const float4 lo4 = make_float4(x[8 * k], x[8 * k + 2], x[8 * k + 4], x[8 * k + 6]), hi4 = make_float4(x[8 * k + 1], x[8 * k + 3], x[8 * k + 5], x[8 * k + 7]);
-          if (pc.whole) {
-            finish(A, pc.first, pc.hk, G, rr, d, lo4, l_run);
-            finish(A, pc.first, pc.hk, G, rr, DH / 2 + d, hi4, l_run);
-          } else {
-            *reinterpret_cast<float4 *>(part + d) = lo4;
-            *reinterpret_cast<float4 *>(part + DH / 2 + d) = hi4;
+        if (in) {
+          const float4 lo4 = make_float4(x[0], x[2], x[4], x[6]), hi4 = make_float4(x[1], x[3], x[5], x[7]);
+#pragma unroll 1
+          for (int k = MODE == FULL ? 0 : half; k < (MODE == FULL ? 2 : half + 1); ++k) {
+            const int d = 4 * l + k * (DH / 2);
+            if (pc.whole) store_out(A, out + d, k == 0 ? lo4 : hi4);
+            else *reinterpret_cast<float4 *>(part + d) = k == 0 ? lo4 : hi4;
           }
         }
         __syncwarp();
       }
-      if (!pc.whole && in && half == 0) *reinterpret_cast<float2 *>(part + DH) = make_float2(m_run, l_run);
+      if (!pc.whole && in && half == 0 && group == 0) *reinterpret_cast<float2 *>(part + DH) = ml;
       fence_before();
+      __syncwarp();
+      if (n > 0 && lane == 0) arrive(&sync.x_empty);
+      if (n > 0) ++pieces;
       tt += n;
     }
     if (!ok) atomicExch(&sync.error, 1);

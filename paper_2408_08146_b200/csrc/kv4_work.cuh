@@ -153,13 +153,8 @@ __device__ __forceinline__ void add4(float4 &v, float f, float4 x) {
   if (f == 0.f) return;                                   // its numbers may be anything
   v.x = fmaf(f, x.x, v.x); v.y = fmaf(f, x.y, v.y); v.z = fmaf(f, x.z, v.z); v.w = fmaf(f, x.w, v.w);
 }
-// dims d .. d + 3 of query row rr (of the rows that share kv head hk): v / sum
-__device__ __forceinline__ void finish(const Kv4Attn &A, int first, int hk, int G, int rr, int d, float4 v, float sum) {
-  const int i = A.by_group(rr);
-  const long long at = (long long)(first + i) * A.out.row + (long long)(hk * G + rr - i * G) * A.out.head + d;
-  // a row that sees nothing or is not in use is 0; one whose sum is NaN stays NaN
-  if (sum == 0.f || (A.rows.slot != nullptr && A.rows.slot[first + i] < 0)) v = make_float4(0.f, 0.f, 0.f, 0.f);
-  else v = make_float4(v.x / sum, v.y / sum, v.z / sum, v.w / sum);
+// four numbers of the output at element `at`
+__device__ __forceinline__ void store_out(const Kv4Attn &A, long long at, float4 v) {
   if (A.out_type == KV4_FP32) {
     *reinterpret_cast<float4 *>(reinterpret_cast<float *>(A.out.p) + at) = v;
   } else if (A.out_type == KV4_FP16) {
@@ -173,6 +168,15 @@ __device__ __forceinline__ void finish(const Kv4Attn &A, int first, int hk, int 
       *reinterpret_cast<uint2 *>(reinterpret_cast<bf16 *>(A.out_lo) + at) = make_uint2(*reinterpret_cast<const uint32_t *>(&c), *reinterpret_cast<const uint32_t *>(&e));
     }
   }
+}
+// dims d .. d + 3 of query row rr (of the rows that share kv head hk): v / sum
+__device__ __forceinline__ void finish(const Kv4Attn &A, int first, int hk, int G, int rr, int d, float4 v, float sum) {
+  const int i = A.by_group(rr);
+  const long long at = (long long)(first + i) * A.out.row + (long long)(hk * G + rr - i * G) * A.out.head + d;
+  // a row that sees nothing or is not in use is 0; one whose sum is NaN stays NaN
+  if (sum == 0.f || (A.rows.slot != nullptr && A.rows.slot[first + i] < 0)) v = make_float4(0.f, 0.f, 0.f, 0.f);
+  else v = make_float4(v.x / sum, v.y / sum, v.z / sum, v.w / sum);
+  store_out(A, at, v);
 }
 
 // Joins the parts of one item.  grid (sequences * tiles, kv heads, blocks of a tile's rows): RB rows a block, JOINERS groups of DH / 4
