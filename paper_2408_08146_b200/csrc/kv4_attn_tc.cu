@@ -2,17 +2,18 @@
 //
 // One CTA per SM walks through its share of the work (kv4_work.cuh): tiles of 128 (token, head) rows of one kv head, keys in tiles
 // of 64.  Per key tile
-//   seven warps take the tiles' granules of 16 keys in turn and expand their codes: shared memory, fp16, in the layouts that
+//   eight warps take the tiles' granules of 16 keys in turn and expand their codes: shared memory, fp16, in the layouts that
 //                            the MMAs read
-//   S[128 x 64]   = Q K^T    tcgen05.mma, A = Q and B = K from tensor and shared memory
+//   S[128 x 64]   = Q K^T    tcgen05.mma, A = Q from tensor memory, B = K
 //   P             = 2^(...)  four warps, a thread per row; P goes where S was, in tensor memory.  Two groups of four take
-//                            the tiles in turn, each with a maximum, a sum and an O of its own, joined at the end
+//                            the tiles in turn, each with a maximum, sums and an O of its own, joined at the end
 //   O[128 x DH]  += P V      tcgen05.mma, A = P from tensor memory, B = V as [key][dim] (MN-major)
+// S and P V are issued by a warp each; three places for S let S of a tile run while the rows work on the two before.
 // With x = zero + scale code = (zero + 8 scale) + scale (code - 8): scale (code - 8) times a power of two is EXACT in fp16 (8 bits by 3),
-// so K and V are expanded without rounding, and the constants of the vectors come in as more columns of the products: four
-// columns of depth for S (Z_r kz_j, both as two fp16 values), two columns of O (sum of p_j zv_j, likewise).  The power of two is
-// chosen for each granule of 16 keys, so that neither large nor small vectors leave fp16's range; for K it is taken off with the
-// scores (a factor per 16 columns), for V it goes into P, relative to the largest power so far.
+// so K and V are expanded without rounding.  The constants zero + 8 scale of the vectors are the rows' business, in fp32: kz_j sum(q) is
+// added to a score, p_j zv_j summed beside p_j.  The power of two is chosen for each granule of 16 keys, so that neither large nor
+// small vectors leave fp16's range; for K it is taken off with the scores (a factor per 16 columns), for V it goes into P, relative
+// to the largest power so far.
 // Dims are in the order in which words unpack: position 2 d of a row is dim d, position 2 d + 1 dim d + DH/2.
 // Rounding: Q one fp16 value with the row's maximum at 2^7 .. 2^8 (exact for bf16 and fp16 queries down to 2^-22 of the row's maximum), P one
 // fp16 value (2^-12); with fp32 queries two of each.  Products and sums are fp32.
@@ -30,21 +31,23 @@ constexpr int TK = 64;                     // keys of a tile
 constexpr int UG = TK / KV4_G;             // granules of a tile
 constexpr int NB = 3;                      // buffers of K and of V
 constexpr int RING = 3;                    // granules on their way per expanding warp
-constexpr int INFO = 8;                    // tiles whose powers of two are kept (expanding runs at most NB + 3 tiles ahead of the rows)
+constexpr int INFO = 16;                   // tiles whose parameters are kept (expanding runs at most 7 tiles ahead of the rows)
 constexpr int BLK = TK * 128;              // [64 keys][64 dims]
-constexpr int ROW_WARPS = 8, EXPANDERS = 7, MMA_WARP = ROW_WARPS + EXPANDERS;
-constexpr int THREADS = 32 * (MMA_WARP + 1);        // sixteen warps: 128 registers a thread
+constexpr int ROW_WARPS = 8, EXPANDERS = 8, S_WARP = ROW_WARPS + EXPANDERS, PV_WARP = S_WARP + 1;
+constexpr int THREADS = 32 * (S_WARP + 4);          // whole warpgroups, so that registers can be split
+// Registers a thread: 640 threads start with 96 each, 61440 together; 256 x 128 + 256 x 72 + 128 x 72 = 60416.
+constexpr int REGS_START = 96, REGS_ROWS = 128, REGS_EXPAND = 72, REGS_MMA = 72;
+static_assert(32 * (ROW_WARPS * REGS_ROWS + EXPANDERS * REGS_EXPAND + 4 * REGS_MMA) <= THREADS * REGS_START, "the shares fit in what the block starts with");
 constexpr int E_TIMEOUT = 6;
 constexpr float RAISE = 4.f;
 constexpr int P_TOP = 10;                  // P = 2^P_TOP at the reference maximum
-constexpr int COL_S = 0, COL_O = 2 * TK, O_COLS = 144, COL_Q = COL_O + 2 * O_COLS;
+constexpr int COL_S = 0, COL_O = NB * TK, O_COLS = 128, COL_Q = COL_O + 2 * O_COLS;      // + 64 = 512
 constexpr int TMEM_COLS = 512;
 
 enum { FULL = 0, HALF = 1, PAIR = 2 };     // 128 rows; 64 rows twice; 64 rows as two values
 template <int MODE> constexpr int TILE_ROWS = MODE == FULL ? 128 : 64;
 template <int DH> struct Lay {
-  static constexpr int NBLK = DH / 64 + 1;                   // blocks of 64 dims, and the constants
-  static constexpr int ONE = NBLK * BLK;
+  static constexpr int ONE = DH / 64 * BLK;
   static constexpr int K = 0, V = NB * ONE, CODES = 2 * NB * ONE;
   static constexpr int PART = kv4_granule_bytes(DH);
   static constexpr int Q = CODES + EXPANDERS * RING * PART;  // rows of queries as they come: 128 of 16 bits, or 64 of 32
@@ -55,10 +58,11 @@ template <int DH> constexpr unsigned SMEM = Lay<DH>::BYTES + 1024;
 struct TileInfo {
   float k_back[UG];                        // what a score of the granule is multiplied with
   int v_exp[UG];                           // V of the granule was divided by 2^v_exp
+  float kz[TK], zv[TK];                    // the vectors' constants
   unsigned poison[UG], poison_v[UG];       // slots whose K / V is NaN
 };
 struct alignas(16) Sync {
-  uint64_t q_in, q_full, k_full[NB], k_empty[NB], v_full[NB], v_empty[NB], s_full[2], p_full[2], pv_done[2], info_full[INFO], x_full, x_empty, drain;
+  uint64_t q_in, q_full, k_full[NB], v_full[NB], s_done[NB], pv_done[NB], p_full[4], info_full[INFO], x_full, x_empty, drain;
   uint32_t tmem;
   int error;
   TileInfo info[INFO];
@@ -188,28 +192,22 @@ __global__ void __launch_bounds__(THREADS, 1) kv4_attn_tc_kernel(const Kv4Attn A
     mbar_init(&sync.q_in, ROW_WARPS);
     mbar_init(&sync.q_full, ROW_WARPS);
     for (int i = 0; i < NB; ++i) {
-      mbar_init(&sync.k_full[i], UG); mbar_init(&sync.k_empty[i], 1);
-      mbar_init(&sync.v_full[i], UG); mbar_init(&sync.v_empty[i], 1);
+      mbar_init(&sync.k_full[i], UG); mbar_init(&sync.s_done[i], 1);
+      mbar_init(&sync.v_full[i], UG); mbar_init(&sync.pv_done[i], 1);
     }
-    for (int i = 0; i < 2; ++i) { mbar_init(&sync.s_full[i], 1); mbar_init(&sync.p_full[i], ROW_WARPS / 2); mbar_init(&sync.pv_done[i], 1); }
+    for (int i = 0; i < 4; ++i) mbar_init(&sync.p_full[i], ROW_WARPS / 2);
     for (int i = 0; i < INFO; ++i) mbar_init(&sync.info_full[i], UG);
     mbar_init(&sync.x_full, ROW_WARPS);
     mbar_init(&sync.x_empty, ROW_WARPS);
-    mbar_init(&sync.drain, 1);
+    mbar_init(&sync.drain, 2);
     sync.error = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   pdl_wait();                              // before the allocation: the launch before may not have made its own yet
-  if (warp == MMA_WARP) {
+  if (warp == PV_WARP) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sync.tmem)), "r"((uint32_t)TMEM_COLS) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
-  // the second 16 bytes of the constants' rows stay zero
-  for (int e = threadIdx.x; e < 2 * NB * TK; e += THREADS) {
-    const int key = e % TK;
-    sts128(sb + (uint32_t)(e / TK * LY::ONE + (LY::NBLK - 1) * BLK + key * 128 + ((1 ^ (key & 7)) << 4)), 0u, 0u, 0u, 0u);
-  }
-  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   fence_before();
   __syncthreads();
   fence_after();
@@ -222,7 +220,8 @@ __global__ void __launch_bounds__(THREADS, 1) kv4_attn_tc_kernel(const Kv4Attn A
   int tt = 0;                              // tiles before this piece (of this CTA)
   bool ok = true;
 
-  if (warp >= ROW_WARPS && warp < MMA_WARP) {
+  if (warp >= ROW_WARPS && warp < S_WARP) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_EXPAND));
     // ------------------------------------------------------------------ expanding warps
     const int w = warp - ROW_WARPS, g = lane >> 2, t = lane & 3;
     const uint32_t codes = sb + LY::CODES + (uint32_t)(w * RING * LY::PART);
@@ -246,7 +245,6 @@ __global__ void __launch_bounds__(THREADS, 1) kv4_attn_tc_kernel(const Kv4Attn A
     const int ps = lane & 15;
     const bool pv = lane >= 16;
     const uint32_t p_from = (uint32_t)(KV4_G * DH + (ps & 7) * 16 + (pv ? 8 : 0) + (ps >> 3) * 4);
-    const uint32_t p_to = sb + (uint32_t)((pv ? LY::V : LY::K) + (LY::NBLK - 1) * BLK + ps * 128 + ((ps & 7) << 4));
     while (more && ok && walk.next(A, G, lane, pc)) {
       const int n = pc.hi - pc.lo, kv = min(pc.kv, pc.hi * TK), cache_row = A.rows.cache_of(pc.b);
       uint64_t or0 = ~0ull, or1 = ~0ull;   // slots behind ctx that some row sees
@@ -314,15 +312,16 @@ __global__ void __launch_bounds__(THREADS, 1) kv4_attn_tc_kernel(const Kv4Attn A
         const bool finite = fabsf(zc) < INFINITY && sc < INFINITY;
         const unsigned poison = __ballot_sync(0xffffffffu, v && !finite);
         if (!v || !finite) { sc = 0.f; zc = 0.f; }
-        float most = fmaxf(8.f * sc, fabsf(zc));
-#pragma unroll
-        for (int o = 1; o < 16; o <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
-        const int ex = most > 0.f ? max(-112, (int)(__float_as_uint(most) >> 23) - 127) : 13;      // most in [2^ex, 2^(ex + 1))
+        // (bits of numbers that are not negative are in their order)
+        const unsigned bits = __float_as_uint(8.f * sc);
+        const unsigned most = pv ? __reduce_max_sync(0xffff0000u, bits) : __reduce_max_sync(0x0000ffffu, bits);
+        const int ex = most != 0u ? max(-112, (int)(most >> 23) - 127) : 13;      // the largest 8 scale is in [2^ex, 2^(ex + 1))
         const float norm = pow2i(13 - ex);
+        TileInfo &f = sync.info[now & (INFO - 1)];
+        (pv ? f.zv : f.kz)[gq * KV4_G + ps] = zc;
         if (ps == 0) {
-          TileInfo &f = sync.info[now & (INFO - 1)];
           if (pv) {
-            f.v_exp[gq] = most > 0.f ? ex - 13 : -200;
+            f.v_exp[gq] = most != 0u ? ex - 13 : -200;
             f.poison_v[gq] = poison >> 16;
           } else {
             f.k_back[gq] = pow2i(ex - 13);
@@ -331,12 +330,11 @@ __global__ void __launch_bounds__(THREADS, 1) kv4_attn_tc_kernel(const Kv4Attn A
         }
         __syncwarp();
         if (lane == 0) arrive(&sync.info_full[now & (INFO - 1)]);
-        const float z = zc * norm, zh = __half2float(__float2half_rn(z));
-        const uint32_t consts = pack2(zh, z - zh), scale2 = pack2(sc * norm, sc * norm);
+        const uint32_t scale2 = pack2(sc * norm, sc * norm);
         // ---- K
         const uint4 c0 = lds128(at + lane * 16), c1 = DH == 128 ? lds128(at + 512 + lane * 16) : c0;
         const __half2 ka = as_half2(__shfl_sync(0xffffffffu, scale2, g)), kb = as_half2(__shfl_sync(0xffffffffu, scale2, g + 8));
-        if (now >= NB) ok = __all_sync(0xffffffffu, mbar_wait(&sync.k_empty[now % NB], (uint32_t)(now / NB - 1) & 1u));
+        if (now >= NB) ok = __all_sync(0xffffffffu, mbar_wait(&sync.s_done[now % NB], (uint32_t)(now / NB - 1) & 1u));
         if (!ok) break;
         auto put = [&](uint32_t word, __half2 s2, uint32_t to) {
           uint32_t x[4];
@@ -352,8 +350,6 @@ __global__ void __launch_bounds__(THREADS, 1) kv4_attn_tc_kernel(const Kv4Attn A
           put(c0.x, ka, k_at[0] + buf); put(c0.y, ka, k_at[1] + buf);
           put(c0.z, kb, k_at[0] + buf + 1024); put(c0.w, kb, k_at[1] + buf + 1024);
         }
-        // the constants: K has them twice side by side (for the two values of Z), V once
-        if (!pv) sts128(p_to + buf, consts, consts, 0u, 0u);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
         if (lane == 0) arrive(&sync.k_full[now % NB]);
@@ -363,7 +359,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv4_attn_tc_kernel(const Kv4Attn A
         __half2 vs[4];
 #pragma unroll
         for (int s = 0; s < 4; ++s) vs[s] = as_half2(__shfl_sync(0xffffffffu, scale2, 16 + 2 * t + (s & 1) + 8 * (s >> 1)));
-        if (now >= NB) ok = __all_sync(0xffffffffu, mbar_wait(&sync.v_empty[now % NB], (uint32_t)(now / NB - 1) & 1u));
+        if (now >= NB) ok = __all_sync(0xffffffffu, mbar_wait(&sync.pv_done[now % NB], (uint32_t)(now / NB - 1) & 1u));
         if (!ok) break;
         if constexpr (DH == 128) {
           put(odd ? d0.y : d0.x, vs[0], v_at[0][0] + buf); put(odd ? d0.x : d0.y, vs[0], v_at[0][DH / 64 - 1] + buf);
@@ -374,7 +370,6 @@ __global__ void __launch_bounds__(THREADS, 1) kv4_attn_tc_kernel(const Kv4Attn A
           put(d0.x, vs[0], v_at[0][0] + buf); put(d0.y, vs[1], v_at[1][0] + buf);
           put(d0.z, vs[2], v_at[0][0] + buf + 1024); put(d0.w, vs[3], v_at[1][0] + buf + 1024);
         }
-        if (pv) sts128(p_to + buf, consts, 0u, 0u, 0u);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
         if (lane == 0) arrive(&sync.v_full[now % NB]);
@@ -383,50 +378,55 @@ __global__ void __launch_bounds__(THREADS, 1) kv4_attn_tc_kernel(const Kv4Attn A
       tt += n;
     }
     if (!ok) atomicExch(&sync.error, 1);
-  } else if (warp == MMA_WARP) {
-    // ------------------------------------------------------------------ MMA issuer
-    const uint32_t idesc_s = (1u << 4) | ((uint32_t)(TK >> 3) << 17) | ((128u >> 4) << 24);                                  // fp32, fp16 x fp16, N = 64
-    const uint32_t idesc_o = (1u << 4) | (1u << 16) | ((uint32_t)((DH + 16) >> 3) << 17) | ((128u >> 4) << 24);               // N = DH + 16, B MN-major
-    const uint32_t leader = lane == 0 ? 1u : 0u;
-    int pieces = 0;
-    while (more && ok && walk.next(A, G, lane, pc)) {
-      const int n = pc.hi - pc.lo;
-      if (n > 0) {
-        auto issue_s = [&](int now) -> bool {
-          if (!__all_sync(0xffffffffu, mbar_wait(&sync.k_full[now % NB], (uint32_t)(now / NB) & 1u))) return false;
+  } else if (warp >= S_WARP) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_MMA));
+    // ------------------------------------------------------------------ MMA issuers: one warp for S, one for P V
+    // A wait, even for what has long happened, costs the issuer 130 cycles and an MMA 50 to 80: with one warp for both a tile took the
+    // 1950 cycles that it spent on two commits, three waits and twelve MMAs in a row.
+    // Everything here is the same in all lanes, and the compiler is told so (a shuffle from lane 0): loops and descriptors stay in uniform
+    // registers, and one lane issues.
+    const uint32_t leader = lane == 0 ? 1u : 0u, tm = __shfl_sync(0xffffffffu, tmem, 0);
+    int tile = 0, buf = 0;                 // tiles issued, and the buffer of the next
+    uint32_t phase = 0u, q_phase = 0u;
+    while (warp <= PV_WARP && more && ok && walk.next(A, G, lane, pc)) {
+      const int n = __shfl_sync(0xffffffffu, pc.hi - pc.lo, 0);
+      if (warp == S_WARP && n > 0) {
+        const uint32_t idesc = (1u << 4) | ((uint32_t)(TK >> 3) << 17) | ((128u >> 4) << 24);                             // fp32, fp16 x fp16, N = 64
+        ok = __all_sync(0xffffffffu, mbar_wait(&sync.q_full, q_phase));
+        q_phase ^= 1u;
+        for (int i = 0; i < n && ok; ++i) {
+          if (tile >= NB) ok = __all_sync(0xffffffffu, mbar_wait(&sync.pv_done[buf], phase ^ 1u));      // P of the tile before in this place has been read
+          ok = ok && __all_sync(0xffffffffu, mbar_wait(&sync.k_full[buf], phase));
+          if (!ok) break;
           fence_after();
-          const uint64_t kb = smem_desc_sw128(sb + LY::K + (uint32_t)(now % NB * LY::ONE));
-          const uint32_t d = tmem + (uint32_t)(COL_S + (now & 1) * TK);
+          const uint64_t kb = smem_desc_sw128(sb + LY::K + (uint32_t)(buf * LY::ONE));
+          const uint32_t d = tm + (uint32_t)(COL_S + buf * TK);
 #pragma unroll
-          for (int k = 0; k < DH / 16 + 1; ++k)             // the last step: the constants
-            umma_ts(leader, d, tmem + (uint32_t)(COL_Q + 8 * k), kb + (uint64_t)(((k >> 2) * BLK >> 4) + 2 * (k & 3)), idesc_s, k ? 1u : 0u);
-          commit(leader, &sync.s_full[now & 1]);
-          commit(leader, &sync.k_empty[now % NB]);
-          return true;
-        };
-        auto issue_pv = [&](int now, bool first) -> bool {
-          if (!__all_sync(0xffffffffu, mbar_wait(&sync.p_full[now & 1], (uint32_t)(now >> 1) & 1u))) return false;
-          if (!__all_sync(0xffffffffu, mbar_wait(&sync.v_full[now % NB], (uint32_t)(now / NB) & 1u))) return false;
+          for (int k = 0; k < DH / 16; ++k) umma_ts(leader, d, tm + (uint32_t)(COL_Q + 8 * k), kb + (uint64_t)(((k >> 2) * BLK >> 4) + 2 * (k & 3)), idesc, k ? 1u : 0u);
+          commit(leader, &sync.s_done[buf]);                // the scores are there, and K's buffer is free
+          ++tile;
+          if (++buf == NB) { buf = 0; phase ^= 1u; }
+        }
+      } else if (warp == PV_WARP && n > 0) {
+        const uint32_t idesc = (1u << 4) | (1u << 16) | ((uint32_t)(DH >> 3) << 17) | ((128u >> 4) << 24);                  // N = DH, B MN-major
+        for (int i = 0; i < n && ok; ++i) {
+          ok = __all_sync(0xffffffffu, mbar_wait(&sync.v_full[buf], phase));
+          ok = ok && __all_sync(0xffffffffu, mbar_wait(&sync.p_full[tile & 3], (uint32_t)(tile >> 2) & 1u));
+          if (!ok) break;
           fence_after();
-          const uint64_t vb = smem_desc_mn_sw128(sb + LY::V + (uint32_t)(now % NB * LY::ONE), BLK, 1024);
-          const uint32_t p = tmem + (uint32_t)(COL_S + (now & 1) * TK), d = tmem + (uint32_t)(COL_O + (now & 1) * O_COLS);
+          const uint64_t vb = smem_desc_mn_sw128(sb + LY::V + (uint32_t)(buf * LY::ONE), BLK, 1024);
+          const uint32_t p = tm + (uint32_t)(COL_S + buf * TK), d = tm + (uint32_t)(COL_O + (tile & 1) * O_COLS);
 #pragma unroll
-          for (int k = 0; k < TK / 16; ++k) umma_ts(leader, d, p + (uint32_t)(8 * k), vb + (uint64_t)(k * 2048 >> 4), idesc_o, (first && k == 0) ? 0u : 1u);
-          commit(leader, &sync.v_empty[now % NB]);
-          commit(leader, &sync.pv_done[now & 1]);
-          return true;
-        };
-        ok = __all_sync(0xffffffffu, mbar_wait(&sync.q_full, (uint32_t)pieces & 1u));
-        for (int i = -1; i < n && ok; ++i) {
-          if (i + 1 < n) ok = issue_s(tt + i + 1);
-          if (i >= 0 && ok) ok = issue_pv(tt + i, i < 2);          // the first of either group
+          for (int k = 0; k < TK / 16; ++k) umma_ts(leader, d, p + (uint32_t)(8 * k), vb + (uint64_t)(k * 2048 >> 4), idesc, (i < 2 && k == 0) ? 0u : 1u);      // (i < 2: the first of either group)
+          commit(leader, &sync.pv_done[buf]);               // V's buffer is free, and P's place; O is complete
+          ++tile;
+          if (++buf == NB) { buf = 0; phase ^= 1u; }
         }
       }
-      if (n > 0) ++pieces;
-      tt += n;
     }
     if (!ok) atomicExch(&sync.error, 1);
   } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_ROWS));
     // ------------------------------------------------------------------ rows
     const int quarter = warp & 3, group = warp >> 2;      // tensor-memory lanes 32 quarter ..; tiles with now % 2 == group
     const int half = MODE == FULL ? 0 : lane >> 4;
@@ -438,7 +438,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv4_attn_tc_kernel(const Kv4Attn A
       const int n = pc.hi - pc.lo, kv = min(pc.kv, pc.hi * TK);
       const int rr = pc.row0 + row, n_rows = pc.count * G, i_row = A.by_group(rr);
       const bool in = rr < n_rows;
-      float m_run = -INFINITY, l_run = 0.f, factor_row = 0.f;
+      float m_run = -INFINITY, l_run = 0.f, z_run = 0.f, factor_row = 0.f, z_row = 0.f;      // z: of the constants, p_j zv_j and sum(q)
       int k_ref = -200;
       bool nan_row = false, have_o = false;
       if (n > 0) {
@@ -512,14 +512,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv4_attn_tc_kernel(const Kv4Attn A
           tmem_st16(mine + (uint32_t)(COL_Q + d0), q);
         }
         factor_row = fminf(log2_scale / up, 3e38f);
-        if (group == 1) {
-          // the row's sum against the constants, as two values (three with two parts: the second lane adds the rest)
-          const float z = sum * up, zh = __half2float(__float2half_rn(z)), zl = __half2float(__float2half_rn(z - zh)), zr = z - zh - zl;
-          uint32_t c[2] = {pack2(zh, zh), pack2(zl, zl)};
-          if (MODE == PAIR && half) { c[0] = pack2(zr, zr); c[1] = 0u; }
-          asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %3, %3, %3, %3, %3};" ::"r"(mine + (uint32_t)(COL_Q + DH / 2)),
-                       "r"(c[0]), "r"(c[1]), "r"(0u) : "memory");
-        }
+        z_row = sum * log2_scale;
         wait_st();
         fence_before();
         __syncwarp();
@@ -533,111 +526,148 @@ __global__ void __launch_bounds__(THREADS, 1) kv4_attn_tc_kernel(const Kv4Attn A
 #pragma unroll 1
       for (int i = (tt & 1) == group ? 0 : 1; i < n && ok; i += 2) {
         const int now = tt + i;
-        ok = __all_sync(0xffffffffu, mbar_wait(&sync.info_full[now & (INFO - 1)], (uint32_t)(now / INFO) & 1u) && mbar_wait(&sync.s_full[group], (uint32_t)(now >> 1) & 1u));
+        ok = __all_sync(0xffffffffu, mbar_wait(&sync.info_full[now & (INFO - 1)], (uint32_t)(now / INFO) & 1u));
         if (!ok) break;
-        fence_after();
         const TileInfo &f = sync.info[now & (INFO - 1)];
-        const uint32_t s_at = mine + (uint32_t)(COL_S + group * TK);
-        float v[NC];
+        const uint32_t s_at = mine + (uint32_t)(COL_S + now % NB * TK);
+        // O and its sums before this tile are in other units from now on: every P V of this group so far has landed, none is issued before
+        // this warp has handed over its P
+        auto rescale = [&](float by) -> bool {
+          if (!have_o) return true;
+          if (!__all_sync(0xffffffffu, mbar_wait(&sync.pv_done[(now - 2) % NB], (uint32_t)((now - 2) / NB) & 1u))) return false;
+          fence_after();
+#pragma unroll 1
+          for (int c = 0; c < DH; c += 16) {
+            uint32_t o[16];
+            tmem_ld16(o_at + (uint32_t)c, o);
+            wait_ld();
+#pragma unroll
+            for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * by);
+            tmem_st16(o_at + (uint32_t)c, o);
+          }
+          wait_st();
+          return true;
+        };
+        const int key0 = (pc.lo + i) * TK;
+        float fk[NG], pg[NG];
+        unsigned any_poison = 0u;
         {
-          uint32_t all[TK];
+          int top_exp = k_ref;
 #pragma unroll
-          for (int c = 0; c < TK; c += 16) tmem_ld16(s_at + (uint32_t)c, all + c);
-          wait_ld();
-          if constexpr (MODE == FULL) {
+          for (int k = 0; k < UG; ++k) {
+            top_exp = max(top_exp, f.v_exp[k]);
+            any_poison |= f.poison[k] | f.poison_v[k];
+          }
+          if (top_exp > k_ref) {           // (the same in all threads)
+            ok = rescale(k_ref - top_exp < -126 ? 0.f : pow2i(k_ref - top_exp));
+            if (!ok) break;
+            k_ref = top_exp;
+          }
 #pragma unroll
-            for (int j = 0; j < NC; ++j) v[j] = __uint_as_float(all[j]);
-          } else {
-#pragma unroll
-            for (int j = 0; j < NC; ++j) {
-              v[j] = __uint_as_float(half ? all[32 + j] : all[j]);
-              if constexpr (MODE == PAIR) v[j] += __shfl_xor_sync(0xffffffffu, __uint_as_float(half ? all[j] : all[32 + j]), 16);
-            }
+          for (int k = 0; k < NG; ++k) {
+            fk[k] = fminf(fmaxf(factor_row * f.k_back[NG * half + k], 1e-37f), 3e38f);
+            pg[k] = pow2i(max(f.v_exp[NG * half + k] - k_ref, -110) + P_TOP);
           }
         }
-        const int key0 = (pc.lo + i) * TK;
-        float fk[NG];
-        int top_exp = -200;
-        unsigned any_poison = 0u;
-#pragma unroll
-        for (int k = 0; k < UG; ++k) {
-          top_exp = max(top_exp, f.v_exp[k]);
-          any_poison |= f.poison[k] | f.poison_v[k];
-        }
-#pragma unroll
-        for (int k = 0; k < NG; ++k) fk[k] = fminf(factor_row * f.k_back[NG * half + k], 3e38f);
-        if (key0 + TK > min(pc.ctx, kv) || any_poison != 0u) {
-          uint64_t see = ones_below(sees_below - key0);
+        const bool masked = key0 + TK > min(pc.ctx, kv) || any_poison != 0u;
+        uint64_t see = ~0ull;
+        if (masked) {
+          see = ones_below(sees_below - key0);
           if (tree) see &= tree_bits(mk0, mk1, key0 - pc.ctx);
           if (any_poison != 0u) {
 #pragma unroll
             for (int k = 0; k < UG; ++k) nan_row = nan_row || (see >> (KV4_G * k) & (f.poison[k] | f.poison_v[k])) != 0ull;
           }
-          const uint32_t see0 = (uint32_t)(see >> (32 * half)), see1 = (uint32_t)(see >> 32);
-#pragma unroll
-          for (int j = 0; j < NC; ++j) v[j] = ((j < 32 ? see0 : see1) >> (j & 31) & 1u) ? v[j] : -INFINITY;
         }
-        float m_t = -INFINITY;
+        ok = __all_sync(0xffffffffu, mbar_wait(&sync.s_done[now % NB], (uint32_t)(now / NB) & 1u));
+        if (!ok) break;
+        fence_after();
+        // 32 scores of this thread: with 128 rows the first or the second half of the tile's, else the lane's own half
+        auto scores = [&](const uint32_t *first, const uint32_t *second, int part, float *v) {
 #pragma unroll
-        for (int k = 0; k < NG; ++k) {
-          float a = max3(v[16 * k], v[16 * k + 1], v[16 * k + 2]), b = max3(v[16 * k + 3], v[16 * k + 4], v[16 * k + 5]);
-          a = max3(a, v[16 * k + 6], v[16 * k + 7]); b = max3(b, v[16 * k + 8], v[16 * k + 9]);
-          a = max3(a, v[16 * k + 10], v[16 * k + 11]); b = max3(b, v[16 * k + 12], v[16 * k + 13]);
-          a = max3(a, v[16 * k + 14], v[16 * k + 15]);
-          m_t = fmaxf(m_t, fmaxf(a, b) * fk[k]);
-        }
-        if (MODE != FULL) m_t = fmaxf(m_t, __shfl_xor_sync(0xffffffffu, m_t, 16));
-        float factor = 1.f;
-        if (m_t > m_run + RAISE) {         // (the first visible key sets it)
-          factor = m_run == -INFINITY ? 0.f : ex2(m_run - m_t);
-          m_run = m_t;
-        }
-        const int k_was = k_ref;
-        k_ref = max(k_ref, top_exp);
-        const bool change = __any_sync(0xffffffffu, factor != 1.f) || k_ref != k_was;
-        l_run *= factor;
-        if (have_o && change) {
-          // the P V of this group's tile before has landed before O is touched; none is issued before this warp has handed over its P
-          ok = __all_sync(0xffffffffu, mbar_wait(&sync.pv_done[group], (uint32_t)((now - 2) >> 1) & 1u));
-          if (!ok) break;
-          fence_after();
-          const float scaled = factor * (k_was - k_ref < -126 ? 0.f : pow2i(k_was - k_ref));
-#pragma unroll 1
-          for (int c = 0; c < DH + 16; c += 16) {
-            uint32_t o[16];
-            tmem_ld16(o_at + (uint32_t)c, o);
-            wait_ld();
-#pragma unroll
-            for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * scaled);
-            tmem_st16(o_at + (uint32_t)c, o);
+          for (int j = 0; j < 32; ++j) {
+            if constexpr (MODE == FULL) v[j] = __uint_as_float(first[j]);
+            else v[j] = __uint_as_float(half ? second[j] : first[j]);
+            if constexpr (MODE == PAIR) v[j] += __shfl_xor_sync(0xffffffffu, __uint_as_float(half ? first[j] : second[j]), 16);
           }
-          wait_st();
-        }
-        const float mu = m_run == -INFINITY ? 0.f : m_run;
-        const f32x2 mu2 = both(-mu, -mu);
+          if (masked) {
+            const uint32_t bits = (uint32_t)(see >> (32 * (MODE == FULL ? part : half)));
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[j] = (bits >> j & 1u) ? v[j] : -INFINITY;
+          }
+        };
+        // The reference maximum is taken as it stands, and the scores' maximum looked for beside the exponentials; where one exceeds the
+        // reference by more than 2^RAISE (or is the first that the row sees) the reference is raised and the tile done again.
         uint32_t p[NC / 2], p_lo[MODE == PAIR ? NC / 2 : 1];
-        f32x2 l2[2] = {both(l_run, 0.f), both(0.f, 0.f)};
+        f32x2 l2[2], z2[2];
+        const f32x2 zr2 = both(z_row, z_row);
+        bool again;
+        do {
+          const float mu = m_run == -INFINITY ? 0.f : m_run;
+          const f32x2 mu2 = both(-mu, -mu);
+          l2[0] = l2[1] = z2[0] = z2[1] = both(0.f, 0.f);
+          float top2[2] = {-INFINITY, -INFINITY};
+          auto exponentials = [&](const float *v, int part) {
 #pragma unroll
-        for (int k = 0; k < NG; ++k) {
-          const float pg = pow2i(max(f.v_exp[NG * half + k] - k_ref, -110) + P_TOP);
-          const f32x2 pg2 = both(pg, pg), fk2 = both(fk[k], fk[k]);
+            for (int k = 0; k < 2; ++k) {
+              const int gk = 2 * part + k;
+              const f32x2 pg2 = both(pg[gk], pg[gk]), fk2 = both(fk[gk], fk[gk]);
 #pragma unroll
-          for (int j = 0; j < 16; j += 2) {
-            const float2 e = apart(fma2(both(v[16 * k + j], v[16 * k + j + 1]), fk2, mu2));
-            const f32x2 ab = both(ex2(e.x), ex2(e.y));
-            l2[(j >> 1) & 1] = add2(l2[(j >> 1) & 1], ab);
-            const float2 w = apart(mul2(ab, pg2));
-            const uint32_t h = pack2(w.x, w.y);
-            p[8 * k + j / 2] = h;
-            if constexpr (MODE == PAIR) {
-              const float2 back = unpack2(h);
-              p_lo[8 * k + j / 2] = pack2(w.x - back.x, w.y - back.y);
+              for (int j = 0; j < 16; j += 2) {
+                const int at = MODE == FULL ? 16 * gk + j : 32 * half + 16 * k + j;
+                const f32x2 kz2 = *reinterpret_cast<const f32x2 *>(f.kz + at), zv2 = *reinterpret_cast<const f32x2 *>(f.zv + at);
+                const float2 e = apart(fma2(both(v[16 * k + j], v[16 * k + j + 1]), fk2, fma2(kz2, zr2, mu2)));
+                top2[(j >> 1) & 1] = max3(top2[(j >> 1) & 1], e.x, e.y);
+                const f32x2 ab = both(ex2(e.x), ex2(e.y));
+                l2[(j >> 1) & 1] = add2(l2[(j >> 1) & 1], ab);
+                z2[(j >> 1) & 1] = fma2(ab, zv2, z2[(j >> 1) & 1]);
+                const float2 w = apart(mul2(ab, pg2));
+                const uint32_t h = pack2(w.x, w.y);
+                p[8 * gk + j / 2] = h;
+                if constexpr (MODE == PAIR) {
+                  const float2 back = unpack2(h);
+                  p_lo[8 * gk + j / 2] = pack2(w.x - back.x, w.y - back.y);
+                }
+              }
             }
+          };
+          uint32_t s0[32], s1[32];
+          float v[32];
+          tmem_ld16(s_at, s0);
+          tmem_ld16(s_at + 16u, s0 + 16);
+          if (MODE == FULL) wait_ld();
+          tmem_ld16(s_at + 32u, s1);
+          tmem_ld16(s_at + 48u, s1 + 16);
+          if (MODE != FULL) wait_ld();
+          scores(s0, s1, 0, v);
+          exponentials(v, 0);
+          if constexpr (MODE == FULL) {
+            wait_ld();
+            scores(s1, s1, 1, v);
+            exponentials(v, 1);
           }
-        }
+          float over = fmaxf(top2[0], top2[1]);
+          if (MODE != FULL) over = fmaxf(over, __shfl_xor_sync(0xffffffffu, over, 16));
+          const bool raise = over > (m_run == -INFINITY ? -INFINITY : RAISE);
+          again = __any_sync(0xffffffffu, raise);
+          if (again) {
+            float factor = 1.f;
+            if (raise) {
+              factor = m_run == -INFINITY ? 0.f : ex2(-over);
+              m_run = mu + over;
+            }
+            l_run *= factor;
+            z_run *= factor;
+            ok = rescale(factor);
+            if (!ok) break;
+          }
+        } while (again);
+        if (!ok) break;
         {
           const float2 s = apart(add2(l2[0], l2[1]));
-          l_run = s.x + s.y;
+          l_run += s.x + s.y;
+          const float2 z = apart(add2(z2[0], z2[1]));
+          z_run += z.x + z.y;
         }
         __syncwarp();
         // ---- P where S was: every lane of this warp has read its S
@@ -663,29 +693,30 @@ __global__ void __launch_bounds__(THREADS, 1) kv4_attn_tc_kernel(const Kv4Attn A
         wait_st();
         fence_before();
         __syncwarp();
-        if (lane == 0) arrive(&sync.p_full[group]);
+        if (lane == 0) arrive(&sync.p_full[now & 3]);
         have_o = true;
       }
       if (!ok) break;
       // ---- the piece's result: both groups' products have landed
       if (n > 0) {
         const int last = tt + n - 1, last_other = last - 1;
-        ok = __all_sync(0xffffffffu, mbar_wait(&sync.pv_done[last & 1], (uint32_t)(last >> 1) & 1u) &&
-                                         (n < 2 || mbar_wait(&sync.pv_done[last_other & 1], (uint32_t)(last_other >> 1) & 1u)));
+        ok = __all_sync(0xffffffffu, mbar_wait(&sync.pv_done[last % NB], (uint32_t)(last / NB) & 1u) &&
+                                         (n < 2 || mbar_wait(&sync.pv_done[last_other % NB], (uint32_t)(last_other / NB) & 1u)));
         if (!ok) break;
         fence_after();
       }
       if (MODE != FULL) {
         l_run += __shfl_xor_sync(0xffffffffu, l_run, 16);
+        z_run += __shfl_xor_sync(0xffffffffu, z_run, 16);
         const int other = __shfl_xor_sync(0xffffffffu, nan_row ? 1 : 0, 16);      // (by every lane, whatever it has itself)
         nan_row = nan_row || other != 0;
       }
       if (nan_row) l_run = NAN;
       // ---- the groups together: group 0 writes the first half of the dims' words, group 1 the second
       float2 ml = make_float2(m_run, l_run);
-      float unit[2] = {0.f, 0.f};
+      float unit[2] = {0.f, 0.f}, zs = 0.f;
       if (n > 0) {
-        if (half == 0) sync.x[group][row] = make_float4(m_run, l_run, have_o ? exp2f((float)(k_ref - P_TOP)) : 0.f, 0.f);
+        if (half == 0) sync.x[group][row] = make_float4(m_run, l_run, have_o ? exp2f((float)(k_ref - P_TOP)) : 0.f, z_run);
         __syncwarp();
         if (lane == 0) arrive(&sync.x_full);
         ok = __all_sync(0xffffffffu, mbar_wait(&sync.x_full, (uint32_t)pieces & 1u));
@@ -695,20 +726,14 @@ __global__ void __launch_bounds__(THREADS, 1) kv4_attn_tc_kernel(const Kv4Attn A
         ml = make_float2(top, (x0.x == -INFINITY ? x0.y : f0 * x0.y) + (x1.x == -INFINITY ? x1.y : f1 * x1.y));
         unit[0] = x0.z * f0;
         unit[1] = x1.z * f1;
+        zs = (f0 != 0.f ? f0 * x0.w : 0.f) + (f1 != 0.f ? f1 * x1.w : 0.f);
       }
       const float inv = !pc.whole ? 1.f : ml.y != 0.f && (used || !in) ? 1.f / ml.y : 0.f;      // nothing seen, or not in use: 0
       float *part = part_of<DH, ROWS>(scratch, blockIdx.x, pc.begins) + row * PART_ROW<DH>;
       const long long out = in ? (long long)(pc.first + i_row) * A.out.row + (long long)(pc.hk * G + rr - i_row * G) * A.out.head : 0;
-      float zs[2];
-#pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        uint32_t o[8];
-        tmem_ld8(mine + (uint32_t)(COL_O + k * O_COLS + DH), o);
-        wait_ld();
-        zs[k] = __uint_as_float(o[0]) + __uint_as_float(o[1]);
-        if (MODE != FULL) zs[k] += __shfl_xor_sync(0xffffffffu, zs[k], 16);
-        unit[k] *= inv;
-      }
+      unit[0] *= inv;
+      unit[1] *= inv;
+      zs *= inv;
 #pragma unroll 1
       for (int l = group * (DH / 16); l < (group + 1) * (DH / 16); ++l) {      // words: dims 4l .. 4l + 3 and DH/2 + 4l ..
         uint32_t o[2][8];
@@ -718,12 +743,12 @@ __global__ void __launch_bounds__(THREADS, 1) kv4_attn_tc_kernel(const Kv4Attn A
         float x[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          x[j] = 0.f;
+          x[j] = zs;
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
             float a = __uint_as_float(o[k][j]);
             if (MODE != FULL) a += __shfl_xor_sync(0xffffffffu, a, 16);
-            if (unit[k] != 0.f) x[j] = fmaf(a + zs[k], unit[k], x[j]);         // (an O that was never written may hold anything)
+            if (unit[k] != 0.f) x[j] = fmaf(a, unit[k], x[j]);         // (an O that was never written may hold anything)
           }
         }
         if (in) {
@@ -750,12 +775,10 @@ __global__ void __launch_bounds__(THREADS, 1) kv4_attn_tc_kernel(const Kv4Attn A
   fence_before();
   __syncthreads();
   const bool failed = sync.error != 0;
-  if (warp == MMA_WARP) {
-    // MMAs issued before a wait ran out may still be running: no free under them
-    if (failed && lane == 0) {
-      umma_commit(&sync.drain);
-      (void)mbar_wait(&sync.drain, 0);
-    }
+  // MMAs issued before a wait ran out may still be running: no free under them
+  if (failed && (warp == S_WARP || warp == PV_WARP) && lane == 0) umma_commit(&sync.drain);
+  if (warp == PV_WARP) {
+    if (failed && lane == 0) (void)mbar_wait(&sync.drain, 0);
     __syncwarp();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)TMEM_COLS) : "memory");
   }
