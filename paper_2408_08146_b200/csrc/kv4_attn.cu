@@ -497,8 +497,7 @@ template <int DH, int NT, bool PAIR> cudaError_t go(Launch L, const Kv4Attn &a, 
   const int grid = kv4_attention_ctas(num_sms, NT);
   e = launch_k(kv4_attn_kernel<DH, NT, PAIR>, dim3(grid), dim3(32 * WARPS), RING<DH, NT>, L.st, L.pdl, a, a.scratch, tiles);
   if (e != cudaSuccess) return e;
-  return launch_k(kv4_join_kernel<DH, 8 * NT, 1, 1, 16>, dim3(a.rows.B * tiles, a.c.n_kv_heads, rows < 8 * NT ? rows : 8 * NT), dim3(DH / 4 * 16), 0, L.st,
-                  L.pdl, a, a.scratch, tiles, (unsigned)grid);
+  return launch_k(kv4_join_kernel<DH, 8 * NT, 1>, dim3(grid), dim3(JOIN_THREADS), 0, L.st, L.pdl, a, a.scratch, tiles);
 }
 
 }  // namespace

@@ -10,12 +10,12 @@
 //   O[128 x DH]  += P V      tcgen05.mma, A = P from tensor memory, B = V as [key][dim] (MN-major)
 // S and P V are issued by a warp each; three places for S let S of a tile run while the rows work on the two before.
 // With x = zero + scale code = (zero + 8 scale) + scale (code - 8): scale (code - 8) times a power of two is EXACT in fp16 (8 bits by 3),
-// so K and V are expanded without rounding.  The constants zero + 8 scale of the vectors are the rows' business, in fp32: kz_j sum(q) is
+// so K and V are expanded without rounding (a vector whose scale is below 1/32 of its granule's largest: to 2^-20 of that one's values).  The constants zero + 8 scale of the vectors are the rows' business, in fp32: kz_j sum(q) is
 // added to a score, p_j zv_j summed beside p_j.  The power of two is chosen for each granule of 16 keys, so that neither large nor
 // small vectors leave fp16's range; for K it is taken off with the scores (a factor per 16 columns), for V it goes into P, relative
 // to the largest power so far.
 // Dims are in the order in which words unpack: position 2 d of a row is dim d, position 2 d + 1 dim d + DH/2.
-// Rounding: Q one fp16 value with the row's maximum at 2^7 .. 2^8 (exact for bf16 and fp16 queries down to 2^-22 of the row's maximum), P one
+// Rounding: Q one fp16 value with the row's maximum at 2^14 .. 2^15 (exact for bf16 and fp16 queries down to 2^-29 of the row's maximum), P one
 // fp16 value (2^-12); with fp32 queries two of each.  Products and sums are fp32.
 // The form with 64 rows has every row twice, in lanes l and l + 16 of a warp, each with half of the keys to take 2^x of (half the work of the
 // rows); with fp32 queries the two lanes hold the two parts of Q and P.
@@ -120,14 +120,19 @@ __device__ __forceinline__ void sts128(uint32_t at, uint32_t a, uint32_t b, uint
 __device__ __forceinline__ __half2 as_half2(uint32_t v) { return *reinterpret_cast<const __half2 *>(&v); }
 __device__ __forceinline__ uint32_t as_u32(__half2 v) { return *reinterpret_cast<const uint32_t *>(&v); }
 
-// Eight codes as (code - 8) * scale: pairs (nibble i, nibble i + 4).  1024 + code and 1024 + 16 code are fp16 numbers with the code in their bits.
-__device__ __forceinline__ void expand(uint32_t w, __half2 scale, uint32_t *x) {
-  const __half2 back = as_half2(0xe408e408u), sixteenth = as_half2(0x2c002c00u), back16 = as_half2(0xd480d480u);      // -1032, 1/16, -72
+// Waits for two barriers; both are looked at before either answer is used.
+__device__ __forceinline__ bool mbar_wait2(uint64_t *a, uint32_t pa, uint64_t *b, uint32_t pb) {
+  const bool da = mbar_try(smem_u32(a), pa), db = mbar_try(smem_u32(b), pb);
+  return (da || mbar_wait(a, pa)) && (db || mbar_wait(b, pb));
+}
+
+// Eight codes as (code - 8) * scale: pairs (nibble i, nibble i + 4).  A code in the low bits of an fp16 is that number times 2^-24, in bits 4 .. 7
+// 16 times that; mul is scale * 2^24, off -8 scale, and the sum is exact while scale >= 2^-14.
+__device__ __forceinline__ void expand(uint32_t w, __half2 mul, __half2 mul16, __half2 off, uint32_t *x) {
 #pragma unroll
   for (int e = 0; e < 2; ++e) {
-    const uint32_t lo = (w & 0x000f000fu) | 0x64006400u, hi = (w & 0x00f000f0u) | 0x64006400u;
-    x[2 * e] = as_u32(__hmul2(__hadd2(as_half2(lo), back), scale));
-    x[2 * e + 1] = as_u32(__hmul2(__hfma2(as_half2(hi), sixteenth, back16), scale));
+    x[2 * e] = as_u32(__hfma2(as_half2(w & 0x000f000fu), mul, off));
+    x[2 * e + 1] = as_u32(__hfma2(as_half2(w & 0x00f000f0u), mul16, off));
     w >>= 8;
   }
 }
@@ -159,12 +164,6 @@ __device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
   return d;
 }
-__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
-  f32x2 d;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
-
 // rows of a tile of 64 keys that a row sees: bit j is key0 + j
 __device__ __forceinline__ uint64_t ones_below(int n) { return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1ull; }
 __device__ __forceinline__ uint64_t tree_bits(uint64_t m0, uint64_t m1, int shift) {      // shift = key0 - ctx
@@ -315,30 +314,32 @@ __global__ void __launch_bounds__(THREADS, 1) kv4_attn_tc_kernel(const Kv4Attn A
         // (bits of numbers that are not negative are in their order)
         const unsigned bits = __float_as_uint(8.f * sc);
         const unsigned most = pv ? __reduce_max_sync(0xffff0000u, bits) : __reduce_max_sync(0x0000ffffu, bits);
-        const int ex = most != 0u ? max(-112, (int)(most >> 23) - 127) : 13;      // the largest 8 scale is in [2^ex, 2^(ex + 1))
-        const float norm = pow2i(13 - ex);
+        const int ex = most != 0u ? max(-112, (int)(most >> 23) - 127) : -6;      // the largest 8 scale is in [2^ex, 2^(ex + 1))
+        const float norm = pow2i(-6 - ex);                                       // and comes to [2^-6, 2^-5): 2^24 scale stays below 2^16
         TileInfo &f = sync.info[now & (INFO - 1)];
         (pv ? f.zv : f.kz)[gq * KV4_G + ps] = zc;
         if (ps == 0) {
           if (pv) {
-            f.v_exp[gq] = most != 0u ? ex - 13 : -200;
+            f.v_exp[gq] = most != 0u ? ex + 6 : -200;
             f.poison_v[gq] = poison >> 16;
           } else {
-            f.k_back[gq] = pow2i(ex - 13);
+            f.k_back[gq] = pow2i(ex + 6);
             f.poison[gq] = poison & 0xffffu;
           }
         }
         __syncwarp();
         if (lane == 0) arrive(&sync.info_full[now & (INFO - 1)]);
-        const uint32_t scale2 = pack2(sc * norm, sc * norm);
+        const float mul = sc * norm * 16777216.f;
+        const uint32_t scale2 = pack2(mul, -8.f * sc * norm);      // (both exact)
         // ---- K
         const uint4 c0 = lds128(at + lane * 16), c1 = DH == 128 ? lds128(at + 512 + lane * 16) : c0;
-        const __half2 ka = as_half2(__shfl_sync(0xffffffffu, scale2, g)), kb = as_half2(__shfl_sync(0xffffffffu, scale2, g + 8));
+        const uint32_t ka = __shfl_sync(0xffffffffu, scale2, g), kb = __shfl_sync(0xffffffffu, scale2, g + 8);
         if (now >= NB) ok = __all_sync(0xffffffffu, mbar_wait(&sync.s_done[now % NB], (uint32_t)(now / NB - 1) & 1u));
         if (!ok) break;
-        auto put = [&](uint32_t word, __half2 s2, uint32_t to) {
+        auto put = [&](uint32_t word, uint32_t s2, uint32_t to) {
+          const __half2 mul2 = __low2half2(as_half2(s2)), off2 = __high2half2(as_half2(s2));
           uint32_t x[4];
-          expand(word, s2, x);
+          expand(word, mul2, __hmul2(mul2, as_half2(0x2c002c00u)), off2, x);      // 1/16
           sts128(to, x[0], x[1], x[2], x[3]);
         };
         if constexpr (DH == 128) {
@@ -356,9 +357,9 @@ __global__ void __launch_bounds__(THREADS, 1) kv4_attn_tc_kernel(const Kv4Attn A
         // ---- V
         const uint32_t vat = at + KV4_G * DH / 2 + lane * 16;
         const uint4 d0 = lds128(vat), d1 = DH == 128 ? lds128(vat + 512) : d0;
-        __half2 vs[4];
+        uint32_t vs[4];
 #pragma unroll
-        for (int s = 0; s < 4; ++s) vs[s] = as_half2(__shfl_sync(0xffffffffu, scale2, 16 + 2 * t + (s & 1) + 8 * (s >> 1)));
+        for (int s = 0; s < 4; ++s) vs[s] = __shfl_sync(0xffffffffu, scale2, 16 + 2 * t + (s & 1) + 8 * (s >> 1));
         if (now >= NB) ok = __all_sync(0xffffffffu, mbar_wait(&sync.pv_done[now % NB], (uint32_t)(now / NB - 1) & 1u));
         if (!ok) break;
         if constexpr (DH == 128) {
@@ -395,8 +396,8 @@ __global__ void __launch_bounds__(THREADS, 1) kv4_attn_tc_kernel(const Kv4Attn A
         ok = __all_sync(0xffffffffu, mbar_wait(&sync.q_full, q_phase));
         q_phase ^= 1u;
         for (int i = 0; i < n && ok; ++i) {
-          if (tile >= NB) ok = __all_sync(0xffffffffu, mbar_wait(&sync.pv_done[buf], phase ^ 1u));      // P of the tile before in this place has been read
-          ok = ok && __all_sync(0xffffffffu, mbar_wait(&sync.k_full[buf], phase));
+          // (P of the tile before in this place has been read: before the first, a fresh barrier's other phase counts as done)
+          ok = __all_sync(0xffffffffu, mbar_wait2(&sync.pv_done[buf], phase ^ 1u, &sync.k_full[buf], phase));
           if (!ok) break;
           fence_after();
           const uint64_t kb = smem_desc_sw128(sb + LY::K + (uint32_t)(buf * LY::ONE));
@@ -410,8 +411,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv4_attn_tc_kernel(const Kv4Attn A
       } else if (warp == PV_WARP && n > 0) {
         const uint32_t idesc = (1u << 4) | (1u << 16) | ((uint32_t)(DH >> 3) << 17) | ((128u >> 4) << 24);                  // N = DH, B MN-major
         for (int i = 0; i < n && ok; ++i) {
-          ok = __all_sync(0xffffffffu, mbar_wait(&sync.v_full[buf], phase));
-          ok = ok && __all_sync(0xffffffffu, mbar_wait(&sync.p_full[tile & 3], (uint32_t)(tile >> 2) & 1u));
+          ok = __all_sync(0xffffffffu, mbar_wait2(&sync.v_full[buf], phase, &sync.p_full[tile & 3], (uint32_t)(tile >> 2) & 1u));
           if (!ok) break;
           fence_after();
           const uint64_t vb = smem_desc_mn_sw128(sb + LY::V + (uint32_t)(buf * LY::ONE), BLK, 1024);
@@ -490,7 +490,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv4_attn_tc_kernel(const Kv4Attn A
             sum += (x[k].x + x[k].y) + (x[k].z + x[k].w);
           }
         }
-        const float up = pow2i(7 - max(-112, min((int)(__float_as_uint(top) >> 23) - 127, 126)));
+        const float up = pow2i(14 - max(-112, min((int)(__float_as_uint(top) >> 23) - 127, 126)));
 #pragma unroll 1
         for (int c = 0; c < QC; c += 16) {
           uint32_t q[16];
@@ -526,8 +526,9 @@ __global__ void __launch_bounds__(THREADS, 1) kv4_attn_tc_kernel(const Kv4Attn A
 #pragma unroll 1
       for (int i = (tt & 1) == group ? 0 : 1; i < n && ok; i += 2) {
         const int now = tt + i;
-        ok = __all_sync(0xffffffffu, mbar_wait(&sync.info_full[now & (INFO - 1)], (uint32_t)(now / INFO) & 1u));
+        ok = __all_sync(0xffffffffu, mbar_wait2(&sync.info_full[now & (INFO - 1)], (uint32_t)(now / INFO) & 1u, &sync.s_done[now % NB], (uint32_t)(now / NB) & 1u));
         if (!ok) break;
+        fence_after();
         const TileInfo &f = sync.info[now & (INFO - 1)];
         const uint32_t s_at = mine + (uint32_t)(COL_S + now % NB * TK);
         // O and its sums before this tile are in other units from now on: every P V of this group so far has landed, none is issued before
@@ -549,7 +550,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv4_attn_tc_kernel(const Kv4Attn A
           return true;
         };
         const int key0 = (pc.lo + i) * TK;
-        float fk[NG], pg[NG];
+        float fk[NG], lp[NG];              // a score's factor; log2 of what a weight is multiplied with
         unsigned any_poison = 0u;
         {
           int top_exp = k_ref;
@@ -566,7 +567,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv4_attn_tc_kernel(const Kv4Attn A
 #pragma unroll
           for (int k = 0; k < NG; ++k) {
             fk[k] = fminf(fmaxf(factor_row * f.k_back[NG * half + k], 1e-37f), 3e38f);
-            pg[k] = pow2i(max(f.v_exp[NG * half + k] - k_ref, -110) + P_TOP);
+            lp[k] = (float)(max(f.v_exp[NG * half + k] - k_ref, -60) + P_TOP);
           }
         }
         const bool masked = key0 + TK > min(pc.ctx, kv) || any_poison != 0u;
@@ -579,9 +580,6 @@ __global__ void __launch_bounds__(THREADS, 1) kv4_attn_tc_kernel(const Kv4Attn A
             for (int k = 0; k < UG; ++k) nan_row = nan_row || (see >> (KV4_G * k) & (f.poison[k] | f.poison_v[k])) != 0ull;
           }
         }
-        ok = __all_sync(0xffffffffu, mbar_wait(&sync.s_done[now % NB], (uint32_t)(now / NB) & 1u));
-        if (!ok) break;
-        fence_after();
         // 32 scores of this thread: with 128 rows the first or the second half of the tile's, else the lane's own half
         auto scores = [&](const uint32_t *first, const uint32_t *second, int part, float *v) {
 #pragma unroll
@@ -599,29 +597,31 @@ __global__ void __launch_bounds__(THREADS, 1) kv4_attn_tc_kernel(const Kv4Attn A
         // The reference maximum is taken as it stands, and the scores' maximum looked for beside the exponentials; where one exceeds the
         // reference by more than 2^RAISE (or is the first that the row sees) the reference is raised and the tile done again.
         uint32_t p[NC / 2], p_lo[MODE == PAIR ? NC / 2 : 1];
-        f32x2 l2[2], z2[2];
+        float l_new, z_new;
         const f32x2 zr2 = both(z_row, z_row);
         bool again;
         do {
           const float mu = m_run == -INFINITY ? 0.f : m_run;
-          const f32x2 mu2 = both(-mu, -mu);
-          l2[0] = l2[1] = z2[0] = z2[1] = both(0.f, 0.f);
-          float top2[2] = {-INFINITY, -INFINITY};
+          float over = -INFINITY;          // the scores' maximum above the reference
+          l_new = z_new = 0.f;
           auto exponentials = [&](const float *v, int part) {
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
               const int gk = 2 * part + k;
-              const f32x2 pg2 = both(pg[gk], pg[gk]), fk2 = both(fk[gk], fk[gk]);
+              const float base = lp[gk] - mu;
+              const f32x2 base2 = both(base, base), fk2 = both(fk[gk], fk[gk]);
+              f32x2 lg = both(0.f, 0.f), zg = both(0.f, 0.f);
+              float most = -INFINITY;
 #pragma unroll
               for (int j = 0; j < 16; j += 2) {
                 const int at = MODE == FULL ? 16 * gk + j : 32 * half + 16 * k + j;
                 const f32x2 kz2 = *reinterpret_cast<const f32x2 *>(f.kz + at), zv2 = *reinterpret_cast<const f32x2 *>(f.zv + at);
-                const float2 e = apart(fma2(both(v[16 * k + j], v[16 * k + j + 1]), fk2, fma2(kz2, zr2, mu2)));
-                top2[(j >> 1) & 1] = max3(top2[(j >> 1) & 1], e.x, e.y);
-                const f32x2 ab = both(ex2(e.x), ex2(e.y));
-                l2[(j >> 1) & 1] = add2(l2[(j >> 1) & 1], ab);
-                z2[(j >> 1) & 1] = fma2(ab, zv2, z2[(j >> 1) & 1]);
-                const float2 w = apart(mul2(ab, pg2));
+                const float2 e = apart(fma2(both(v[16 * k + j], v[16 * k + j + 1]), fk2, fma2(kz2, zr2, base2)));
+                most = max3(most, e.x, e.y);
+                const float2 w = make_float2(ex2(e.x), ex2(e.y));
+                const f32x2 w2 = both(w.x, w.y);
+                lg = add2(lg, w2);
+                zg = fma2(w2, zv2, zg);
                 const uint32_t h = pack2(w.x, w.y);
                 p[8 * gk + j / 2] = h;
                 if constexpr (MODE == PAIR) {
@@ -629,6 +629,11 @@ __global__ void __launch_bounds__(THREADS, 1) kv4_attn_tc_kernel(const Kv4Attn A
                   p_lo[8 * gk + j / 2] = pack2(w.x - back.x, w.y - back.y);
                 }
               }
+              const float un = pow2i(-(int)lp[gk]);
+              const float2 ls = apart(lg), zz = apart(zg);
+              l_new = fmaf(ls.x + ls.y, un, l_new);
+              z_new = fmaf(zz.x + zz.y, un, z_new);
+              over = fmaxf(over, most - lp[gk]);
             }
           };
           uint32_t s0[32], s1[32];
@@ -646,7 +651,6 @@ __global__ void __launch_bounds__(THREADS, 1) kv4_attn_tc_kernel(const Kv4Attn A
             scores(s1, s1, 1, v);
             exponentials(v, 1);
           }
-          float over = fmaxf(top2[0], top2[1]);
           if (MODE != FULL) over = fmaxf(over, __shfl_xor_sync(0xffffffffu, over, 16));
           const bool raise = over > (m_run == -INFINITY ? -INFINITY : RAISE);
           again = __any_sync(0xffffffffu, raise);
@@ -663,12 +667,8 @@ __global__ void __launch_bounds__(THREADS, 1) kv4_attn_tc_kernel(const Kv4Attn A
           }
         } while (again);
         if (!ok) break;
-        {
-          const float2 s = apart(add2(l2[0], l2[1]));
-          l_run += s.x + s.y;
-          const float2 z = apart(add2(z2[0], z2[1]));
-          z_run += z.x + z.y;
-        }
+        l_run += l_new;
+        z_run += z_new;
         __syncwarp();
         // ---- P where S was: every lane of this warp has read its S
         if constexpr (MODE == FULL) {
@@ -789,13 +789,12 @@ template <int DH, int MODE> cudaError_t go(Launch L, const Kv4Attn &a, int num_s
   static SmemOptIn optin;
   cudaError_t e = optin.ensure((const void *)kv4_attn_tc_kernel<DH, MODE>, SMEM<DH>);
   if (e != cudaSuccess) return e;
-  constexpr int ROWS = TILE_ROWS<MODE>, RB = 8, JOINERS = 2;
+  constexpr int ROWS = TILE_ROWS<MODE>;
   const int rows = a.rows.max_rows * (a.n_heads / a.c.n_kv_heads), tiles = (rows + ROWS - 1) / ROWS;
   e = launch_k(kv4_attn_tc_kernel<DH, MODE>, dim3(num_sms), dim3(THREADS), SMEM<DH>, L.st, L.pdl, a, a.scratch, tiles);
   if (e != cudaSuccess) return e;
   const int in_tile = rows < ROWS ? rows : ROWS;
-  return launch_k(kv4_join_kernel<DH, ROWS, UG, RB, JOINERS>, dim3(a.rows.B * tiles, a.c.n_kv_heads, (in_tile + RB - 1) / RB), dim3(DH / 4 * RB * JOINERS), 0,
-                  L.st, L.pdl, a, a.scratch, tiles, (unsigned)num_sms);
+  return launch_k(kv4_join_kernel<DH, ROWS, UG>, dim3(num_sms, (in_tile + JOIN_ROWS - 1) / JOIN_ROWS), dim3(JOIN_THREADS), 0, L.st, L.pdl, a, a.scratch, tiles);
 }
 
 }  // namespace

@@ -179,56 +179,68 @@ __device__ __forceinline__ void finish(const Kv4Attn &A, int first, int hk, int 
   store_out(A, at, v);
 }
 
-// Joins the parts of one item.  grid (sequences * tiles, kv heads, blocks of a tile's rows): RB rows a block, JOINERS groups of DH / 4
-// threads a row that take its parts in turn, BATCH at a time on their way together.
-template <int DH, int ROWS, int UG, int RB, int JOINERS>
-__global__ void __launch_bounds__(DH / 4 * JOINERS * RB) kv4_join_kernel(const Kv4Attn A, float *scratch, int tiles, unsigned grid) {
-  constexpr int LANES = DH / 4, BATCH = 5;
-  __shared__ float4 acc[RB][JOINERS][LANES];
-  __shared__ float2 ml[RB][JOINERS];
+// Joins the parts of the item that begins in CTA blockIdx.x of the launch before and goes on behind it (there is at most one: a block for each CTA, not for
+// each item, is few blocks whatever the launch).  grid (CTAs, blocks of JOIN_ROWS rows): for each row as many groups of DH / 4 threads
+// as there are, which take its parts in turn, BATCH at a time on their way together.
+constexpr int JOIN_ROWS = 16, JOIN_THREADS = 512;
+template <int DH, int ROWS, int UG>
+__global__ void __launch_bounds__(JOIN_THREADS) kv4_join_kernel(const Kv4Attn A, float *scratch, int tiles) {
+  constexpr int LANES = DH / 4, SLOTS = JOIN_THREADS / LANES, BATCH = 5;
+  __shared__ float4 acc[SLOTS][LANES];
+  __shared__ float2 ml[SLOTS];
   pdl_launch_dependents();
-  const int lane = threadIdx.x & 31, G = A.n_heads / A.c.n_kv_heads;
+  const int lane = threadIdx.x & 31, G = A.n_heads / A.c.n_kv_heads, entries = A.rows.B * tiles;
   const unsigned Hk = (unsigned)A.c.n_kv_heads;
-  const int e = blockIdx.x, hk = blockIdx.y;
-  unsigned long long U = 0, before = 0;
-  Item it;
-  it.span = 0;
-  for (int j = 0; j < A.rows.B * tiles; j += 32) {
-    const Item x = item_of<ROWS, UG>(A, j + lane, tiles, G, false);
-    const unsigned long long n = (unsigned long long)(unsigned)x.span * Hk;
-    U += n;
-    before += j + lane < e ? n : 0ull;
-    if (e >= j && e < j + 32) {
-      it.first = __shfl_sync(0xffffffffu, x.first, e - j);
-      it.count = __shfl_sync(0xffffffffu, x.count, e - j);
-      it.span = __shfl_sync(0xffffffffu, x.span, e - j);
+  const Item near = item_of<ROWS, UG>(A, lane, tiles, G, false);
+  unsigned long long U = (unsigned long long)(unsigned)near.span * Hk;
+  for (int j = 32; j < entries; j += 32) U += (unsigned long long)(unsigned)item_of<ROWS, UG>(A, j + lane, tiles, G, false).span * Hk;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) U += __shfl_xor_sync(0xffffffffu, U, o);
+  const unsigned n = cta_count<ROWS, UG>(U, gridDim.x), c0 = blockIdx.x;
+  int e = 0, hk = 0, first = 0, count = 0;
+  unsigned c1 = c0;
+  if (c0 + 1 < n) {
+    const unsigned long long begin = units_before(U, c0, n), end = units_before(U, c0 + 1, n), u = end - 1;
+    unsigned long long before = 0;
+    for (int j = 0;; j += 32) {                       // (some item has unit u)
+      const Item it = j == 0 ? near : item_of<ROWS, UG>(A, j + lane, tiles, G, false);
+      const unsigned long long units = (unsigned long long)(unsigned)it.span * Hk, upto = before + scan(units, lane);
+      const unsigned hit = __ballot_sync(0xffffffffu, upto > u);
+      if (hit == 0u) {
+        before = __shfl_sync(0xffffffffu, upto, 31);
+        continue;
+      }
+      const int at = __ffs(hit) - 1;
+      e = j + at;
+      first = __shfl_sync(0xffffffffu, it.first, at);
+      count = __shfl_sync(0xffffffffu, it.count, at);
+      const int span = __shfl_sync(0xffffffffu, it.span, at);
+      const unsigned long long start = __shfl_sync(0xffffffffu, upto - units, at);
+      hk = (int)div64(u - start, (unsigned)span);
+      const unsigned long long u0 = start + (unsigned long long)(unsigned)hk * (unsigned)span, u1 = u0 + (unsigned)span;
+      if (u0 >= begin && u1 > end) c1 = cta_of(U, u1 - 1, n);
+      break;
     }
   }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    U += __shfl_xor_sync(0xffffffffu, U, o);
-    before += __shfl_xor_sync(0xffffffffu, before, o);
-  }
   pdl_wait();                              // by every block, whatever it has to do: the launch must not end before the one it joins
-  if (it.span == 0) return;
-  const unsigned n = cta_count<ROWS, UG>(U, grid);
-  const unsigned long long u0 = before + (unsigned long long)(unsigned)hk * (unsigned)it.span;
-  const unsigned c0 = cta_of(U, u0, n), c1 = cta_of(U, u0 + (unsigned)it.span - 1, n);
-  if (c0 == c1) return;
-  const int l = threadIdx.x % LANES, grp = threadIdx.x / LANES % JOINERS, rb = threadIdx.x / (LANES * JOINERS);
-  const int r = blockIdx.z * RB + rb, row = (tiles == 1 ? 0 : e % tiles) * ROWS + r;
-  const bool in = row < it.count * G;
+  const int row0 = (tiles == 1 ? 0 : e % tiles) * ROWS + blockIdx.y * JOIN_ROWS;
+  const int rows = min(JOIN_ROWS, count * G - row0);
+  if (c1 == c0 || rows <= 0) return;
+  int r2 = 1;
+  while (r2 < rows) r2 *= 2;
+  const int l = threadIdx.x % LANES, slot = threadIdx.x / LANES, r = slot & (r2 - 1), grp = slot / r2, groups = SLOTS / r2;
+  const bool in = r < rows;
   float top = -INFINITY, sum = 0.f;
   float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (unsigned c = c0 + grp; in && c <= c1; c += BATCH * JOINERS) {
+  for (unsigned c = c0 + grp; in && c <= c1; c += BATCH * groups) {
     float2 q[BATCH];
     float4 x[BATCH];
 #pragma unroll
     for (int k = 0; k < BATCH; ++k) {
-      const unsigned ck = c + k * JOINERS;
+      const unsigned ck = c + k * groups;
       q[k] = make_float2(-INFINITY, 0.f);
       if (ck > c1) continue;
-      const float *p = part_of<DH, ROWS>(scratch, ck, ck == c0) + r * PART_ROW<DH>;
+      const float *p = part_of<DH, ROWS>(scratch, ck, ck == c0) + (blockIdx.y * JOIN_ROWS + r) * PART_ROW<DH>;
       q[k] = *reinterpret_cast<const float2 *>(p + DH);
       x[k] = *reinterpret_cast<const float4 *>(p + 4 * l);
     }
@@ -246,22 +258,23 @@ __global__ void __launch_bounds__(DH / 4 * JOINERS * RB) kv4_join_kernel(const K
       if (f != 0.f) add4(v, f, x[k]);
     }
   }
-  acc[rb][grp][l] = v;
-  if (l == 0) ml[rb][grp] = make_float2(top, sum);
-  __syncthreads();
-  if (grp != 0 || !in) return;
-  top = -INFINITY;
-  sum = 0.f;
-  v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-  for (int k = 0; k < JOINERS; ++k) top = fmaxf(top, ml[rb][k].x);
-#pragma unroll
-  for (int k = 0; k < JOINERS; ++k) {
-    const float f = share(ml[rb][k], top);
-    sum += ml[rb][k].x == -INFINITY ? ml[rb][k].y : f * ml[rb][k].y;
-    add4(v, f, acc[rb][k][l]);
+  if (groups > 1) {
+    acc[slot][l] = v;
+    if (l == 0) ml[slot] = make_float2(top, sum);
+    __syncthreads();
+    if (grp != 0) return;
+    top = -INFINITY;
+    sum = 0.f;
+    v = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int k = 0; k < groups; ++k) top = fmaxf(top, ml[k * r2 + r].x);
+    for (int k = 0; k < groups; ++k) {
+      const float2 part = ml[k * r2 + r];
+      const float f = share(part, top);
+      sum += part.x == -INFINITY ? part.y : f * part.y;
+      add4(v, f, acc[k * r2 + r][l]);
+    }
   }
-  finish(A, it.first, hk, G, row, 4 * l, v, sum);
+  if (in) finish(A, first, hk, G, row0 + r, 4 * l, v, sum);
 }
 
 }  // namespace
