@@ -51,6 +51,15 @@ bool tensor_ok(const koala_kv4_tensor &t, int dtype) {
 }
 Kv4Tensor tensor_of(const koala_kv4_tensor &t) { return Kv4Tensor{t.data, t.row_stride, t.head_stride}; }
 
+// The attention kernels count their work in 32 bits: for each sequence, kv head and tile of rows a unit per 16 (tiles of 64 rows and more: 64) slots
+// that a table row could name.
+bool too_much(const koala_kv4 *k, const koala_kv4_rows *r, int n_heads) {
+  const long long rows = (long long)r->max_rows * (n_heads / k->n_kv_heads), slots = (long long)r->table_stride * k->page_size;
+  if (rows > MAX_HEAD_ROWS) return true;
+  const long long items = (long long)r->B * k->n_kv_heads, tiles = rows > KV4_FEW_ROWS ? (rows + 63) / 64 : 1, units = rows > KV4_FEW_ROWS ? slots / 64 + 8 : slots / 16 + 16;
+  return items * tiles > (1ll << 31) || items * tiles * units >= (1ll << 32);      // (at most 2^31 times 2^26)
+}
+
 int done(cudaError_t e) { return e == cudaSuccess ? KOALA_OK : KOALA_E_CUDA; }
 
 }  // namespace
@@ -80,9 +89,7 @@ int koala_kv4_append(const koala_kv4 *k, int32_t layer, const koala_kv4_rows *r,
 }
 
 size_t koala_kv4_attention_scratch_bytes(const koala_kv4 *k, const koala_kv4_rows *r, int32_t n_heads) {
-  if (!cache_ok(k) || rows_ok(k, r) != KOALA_OK || n_heads < 1 || n_heads % k->n_kv_heads != 0 || r->total == 0 ||
-      (long long)r->max_rows * (n_heads / k->n_kv_heads) > MAX_HEAD_ROWS)
-    return 0;
+  if (!cache_ok(k) || rows_ok(k, r) != KOALA_OK || n_heads < 1 || n_heads % k->n_kv_heads != 0 || r->total == 0 || too_much(k, r, n_heads)) return 0;
   return kv4_attention_scratch(k->head_dim, NUM_SMS, r->max_rows * (n_heads / k->n_kv_heads));
 }
 
@@ -93,7 +100,7 @@ int koala_kv4_attention(const koala_kv4 *k, int32_t layer, const koala_kv4_rows 
   if (rc != KOALA_OK) return rc;
   if (!tensor_ok(t[0], dtype) || !tensor_ok(t[1], dtype)) return KOALA_E_INVALID;
   if (n_heads < 1 || n_heads > 65536 || n_heads % k->n_kv_heads != 0 || !(scale > 0.f && scale < 1e30f)) return KOALA_E_INVALID;
-  if ((long long)r->max_rows * (n_heads / k->n_kv_heads) > MAX_HEAD_ROWS) return KOALA_E_UNSUPPORTED;
+  if (too_much(k, r, n_heads)) return KOALA_E_UNSUPPORTED;
   if (r->total == 0) return KOALA_OK;
   if (!scratch || scratch_bytes < koala_kv4_attention_scratch_bytes(k, r, n_heads)) return KOALA_E_CAPACITY;
   if (((uintptr_t)scratch & 15u) != 0) return KOALA_E_INVALID;

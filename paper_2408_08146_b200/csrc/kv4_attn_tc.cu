@@ -21,6 +21,8 @@
 // rows); with fp32 queries the two lanes hold the two parts of Q and P.
 // O stays in tensor memory; a row's reference maximum is raised only when a score exceeds it by more than 2^4, then its O is rescaled in place.
 // Every wait is bounded: on expiry the kernel records a timeout in *status and leaves.
+#include <type_traits>
+
 #include "kv4_work.cuh"
 #include "tc_ptx.cuh"
 
@@ -66,6 +68,7 @@ struct alignas(16) Sync {
   uint32_t tmem;
   int error;
   TileInfo info[INFO];
+  float2 q_stat[128];                      // largest magnitude and sum of each row of queries
   float4 x[2][128];                        // the groups' maximum, sum and power of two of each row
 };
 
@@ -76,10 +79,6 @@ __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::be
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t *v) {
-  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-               : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]) : "r"(taddr) : "memory");
-}
 // A from tensor memory.  The whole warp comes here and one lane (`leader`) issues: in a branch that one lane takes, the descriptors would be
 // worked out lane by lane and moved to the uniform registers that the instruction reads, some ten dependent instructions per MMA.
 __device__ __forceinline__ void umma_ts(uint32_t leader, uint32_t d, uint32_t a, uint64_t db, uint32_t idesc, uint32_t accumulate) {
@@ -98,8 +97,8 @@ __device__ __forceinline__ void commit(uint32_t leader, uint64_t *bar) {
       "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(smem_u32(bar)), "r"(leader)
       : "memory");
 }
-__device__ __forceinline__ void copy8(uint32_t dst, const void *src) {
-  asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory");
+__device__ __forceinline__ void sts64(uint32_t at, uint32_t a, uint32_t b) {
+  asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(at), "r"(a), "r"(b) : "memory");
 }
 __device__ __forceinline__ uint2 lds64(uint32_t at) {
   uint2 v;
@@ -444,52 +443,60 @@ __global__ void __launch_bounds__(THREADS, 1) kv4_attn_tc_kernel(const Kv4Attn A
       if (n > 0) {
         // ---- Q into tensor memory: column d holds dims d and d + DH/2; group 0 writes the first half of the columns.  (Short code: it runs
         // once a piece, and fetching it is most of what it takes)
-        // The rows come through shared memory, a warp reading whole rows (read by the threads that own them, every load would touch
-        // 32 lines): eight bytes at a time, piece c of row r at place c ^ (r & 15) (c ^ 2 (r & 7), pairs of places, for fp32).
-        constexpr int ROW_B = DH * (MODE == PAIR ? 4 : 2), PER = ROW_B / 8, WARP_ROWS = ROWS / 4;
+        // A warp reads whole rows (read by the threads that own them, every load would touch 32 lines), finds their maximum and sum,
+        // and leaves them in shared memory: piece c of 8 bytes of row r at place c ^ (r & 15) (fp32: 16 bytes, c ^ (r & 7)).
+        constexpr int ROW_B = DH * (MODE == PAIR ? 4 : 2), WARP_ROWS = ROWS / 4, MINE = WARP_ROWS / 2;
+        constexpr int PER = DH / 4, AT_ONCE = MINE * PER / 32;       // lanes of a row; loads of a lane
         const uint32_t q_rows = sb + LY::Q + (uint32_t)(quarter * WARP_ROWS * ROW_B);
-#pragma unroll 4
-        for (int e = lane; e < WARP_ROWS / 2 * PER; e += 32) {
-          const int r = group * (WARP_ROWS / 2) + e / PER, c = e % PER, rq = pc.row0 + quarter * WARP_ROWS + r;
-          if (rq >= n_rows) continue;
-          const int iq = A.by_group(rq);
-          const unsigned char *src = reinterpret_cast<const unsigned char *>(A.q.p) +
-                                     ((long long)(pc.first + iq) * A.q.row + (long long)(pc.hk * G + rq - iq * G) * A.q.head) * (MODE == PAIR ? 4 : 2) + c * 8;
-          copy8(q_rows + (uint32_t)(r * ROW_B + (c ^ (MODE == PAIR ? 2 * (r & 7) : r & 15)) * 8), src);
-        }
-        asm volatile("cp.async.wait_all;" ::: "memory");
-        __syncwarp();
-        if (lane == 0) arrive(&sync.q_in);
-        ok = __all_sync(0xffffffffu, mbar_wait(&sync.q_in, (uint32_t)pieces & 1u));
-        if (!ok) break;
-        float top = 0.f, sum = 0.f;
-        constexpr int QC = DH / 4;         // columns of a group
         const bool is_bf16 = A.q_type == KV4_BF16;
-        const int r_in = MODE == FULL ? lane : lane & 15;
-        const uint32_t my_row = q_rows + (uint32_t)(r_in * ROW_B);
-        auto four = [&](int d) -> float4 {
-          if (!in) return make_float4(0.f, 0.f, 0.f, 0.f);
+        typedef typename std::conditional<MODE == PAIR, uint4, uint2>::type Raw;
+        Raw raw[AT_ONCE];
+        const int c = lane % PER;
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) {
+          const int r = group * MINE + (k * 32 + lane) / PER, rq = pc.row0 + quarter * WARP_ROWS + r, iq = A.by_group(rq);
+          const long long at = (long long)(pc.first + iq) * A.q.row + (long long)(pc.hk * G + rq - iq * G) * A.q.head + 4 * c;
+          raw[k] = Raw{};
+          if (rq < n_rows) raw[k] = *reinterpret_cast<const Raw *>(reinterpret_cast<const unsigned char *>(A.q.p) + at * (MODE == PAIR ? 4 : 2));
+        }
+        auto parts = [&](const Raw &v) -> float4 {
           if constexpr (MODE == PAIR) {
-            const uint4 v = lds128(my_row + (uint32_t)(((d / 2) ^ (2 * (r_in & 7))) * 8));
             return make_float4(__uint_as_float(v.x), __uint_as_float(v.y), __uint_as_float(v.z), __uint_as_float(v.w));
           } else {
-            const uint2 v = lds64(my_row + (uint32_t)(((d / 4) ^ (r_in & 15)) * 8));
             const float2 a = unpack2(v.x), b = unpack2(v.y);
             return is_bf16 ? make_float4(__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xffff0000u), __uint_as_float(v.y << 16), __uint_as_float(v.y & 0xffff0000u))
                            : make_float4(a.x, a.y, b.x, b.y);
           }
         };
-#pragma unroll 1
-        for (int d = 0; d < DH; d += 32) {
-          float4 x[8];
 #pragma unroll
-          for (int k = 0; k < 8; ++k) x[k] = four(d + 4 * k);
+        for (int k = 0; k < AT_ONCE; ++k) {
+          const int r = group * MINE + (k * 32 + lane) / PER;
+          const float4 x = parts(raw[k]);
+          float most = fmaxf(max3(fabsf(x.x), fabsf(x.y), fabsf(x.z)), fabsf(x.w)), all = (x.x + x.y) + (x.z + x.w);
 #pragma unroll
-          for (int k = 0; k < 8; ++k) {
-            top = fmaxf(max3(top, fabsf(x[k].x), fabsf(x[k].y)), fmaxf(fabsf(x[k].z), fabsf(x[k].w)));
-            sum += (x[k].x + x[k].y) + (x[k].z + x[k].w);
+          for (int o = 1; o < PER; o <<= 1) {
+            most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+            all += __shfl_xor_sync(0xffffffffu, all, o);
           }
+          if (c == 0) sync.q_stat[quarter * WARP_ROWS + r] = make_float2(most, all);
+          if constexpr (MODE == PAIR) sts128(q_rows + (uint32_t)(r * ROW_B + (c ^ (r & 7)) * 16), raw[k].x, raw[k].y, raw[k].z, raw[k].w);
+          else sts64(q_rows + (uint32_t)(r * ROW_B + (c ^ (r & 15)) * 8), raw[k].x, raw[k].y);
         }
+        __syncwarp();
+        if (lane == 0) arrive(&sync.q_in);
+        ok = __all_sync(0xffffffffu, mbar_wait(&sync.q_in, (uint32_t)pieces & 1u));
+        if (!ok) break;
+        constexpr int QC = DH / 4;         // columns of a group
+        const float2 stat = sync.q_stat[row];
+        const float top = stat.x, sum = stat.y;
+        const int r_in = MODE == FULL ? lane : lane & 15;
+        const uint32_t my_row = q_rows + (uint32_t)(r_in * ROW_B);
+        auto four = [&](int d) -> float4 {       // (rows behind the last were taken as 0)
+          Raw v;
+          if constexpr (MODE == PAIR) v = lds128(my_row + (uint32_t)(((d / 4) ^ (r_in & 7)) * 16));
+          else v = lds64(my_row + (uint32_t)(((d / 4) ^ (r_in & 15)) * 8));
+          return parts(v);
+        };
         const float up = pow2i(14 - max(-112, min((int)(__float_as_uint(top) >> 23) - 127, 126)));
 #pragma unroll 1
         for (int c = 0; c < QC; c += 16) {
@@ -735,29 +742,36 @@ __global__ void __launch_bounds__(THREADS, 1) kv4_attn_tc_kernel(const Kv4Attn A
       unit[1] *= inv;
       zs *= inv;
 #pragma unroll 1
-      for (int l = group * (DH / 16); l < (group + 1) * (DH / 16); ++l) {      // words: dims 4l .. 4l + 3 and DH/2 + 4l ..
-        uint32_t o[2][8];
-        tmem_ld8(mine + (uint32_t)(COL_O + 8 * l), o[0]);
-        tmem_ld8(mine + (uint32_t)(COL_O + O_COLS + 8 * l), o[1]);
-        wait_ld();
-        float x[8];
+      for (int c = group * (DH / 2); c < (group + 1) * (DH / 2); c += 32) {    // four words: dims 4l .. 4l + 3 and DH/2 + 4l ..
+        uint32_t o[2][32];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          x[j] = zs;
+        for (int k = 0; k < 2; ++k) {
+          tmem_ld16(mine + (uint32_t)(COL_O + k * O_COLS + c), o[k]);
+          tmem_ld16(mine + (uint32_t)(COL_O + k * O_COLS + c + 16), o[k] + 16);
+        }
+        wait_ld();
+#pragma unroll
+        for (int j = 0; j < 32; ++j) {
+          float x = zs;
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
             float a = __uint_as_float(o[k][j]);
             if (MODE != FULL) a += __shfl_xor_sync(0xffffffffu, a, 16);
-            if (unit[k] != 0.f) x[j] = fmaf(a, unit[k], x[j]);         // (an O that was never written may hold anything)
+            if (unit[k] != 0.f) x = fmaf(a, unit[k], x);         // (an O that was never written may hold anything)
           }
+          o[0][j] = __float_as_uint(x);
         }
         if (in) {
-          const float4 lo4 = make_float4(x[0], x[2], x[4], x[6]), hi4 = make_float4(x[1], x[3], x[5], x[7]);
-#pragma unroll 1
-          for (int k = MODE == FULL ? 0 : half; k < (MODE == FULL ? 2 : half + 1); ++k) {
-            const int d = 4 * l + k * (DH / 2);
-            if (pc.whole) store_out(A, out + d, k == 0 ? lo4 : hi4);
-            else *reinterpret_cast<float4 *>(part + d) = k == 0 ? lo4 : hi4;
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            auto even = [&](int k) { return make_float4(__uint_as_float(o[0][8 * w + k]), __uint_as_float(o[0][8 * w + 2 + k]), __uint_as_float(o[0][8 * w + 4 + k]), __uint_as_float(o[0][8 * w + 6 + k])); };
+            const int d = 4 * (c / 8 + w);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              if (MODE != FULL && k != half) continue;
+              if (pc.whole) store_out(A, out + d + k * (DH / 2), even(k));
+              else *reinterpret_cast<float4 *>(part + d + k * (DH / 2)) = even(k);
+            }
           }
         }
         __syncwarp();

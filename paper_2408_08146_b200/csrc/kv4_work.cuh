@@ -4,7 +4,7 @@
 // item: START units for beginning (queries, first pages, the sums at the end), and one unit for every UG granules of keys that some row of
 // the tile sees.  All units stand in one line, sequence by sequence, tile by tile, head by head; CTA c of n takes units [U c / n, U (c + 1) / n).  So
 // every CTA has the same work whatever the lengths, which only the device knows.  An item that lies in several CTAs leaves
-// parts (O, maximum, sum) that a second kernel joins in CTA order.
+// parts (O, maximum, sum) that a second kernel joins in CTA order.  Units are counted in 32 bits (kv4_attention refuses tables that could hold more).
 #pragma once
 #include <cuda_fp16.h>
 
@@ -43,28 +43,24 @@ template <int ROWS, int UG> __device__ __forceinline__ Item item_of(const Kv4Att
   return s;
 }
 
-__device__ __forceinline__ unsigned long long scan(unsigned long long v, int lane) {      // inclusive
+__device__ __forceinline__ unsigned scan(unsigned v, int lane) {      // inclusive
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const unsigned long long x = __shfl_up_sync(0xffffffffu, v, o);
+    const unsigned x = __shfl_up_sync(0xffffffffu, v, o);
     if (lane >= o) v += x;
   }
   return v;
 }
-// a / b where a is mostly below 2^32
-__device__ __forceinline__ unsigned long long div64(unsigned long long a, unsigned b) {
-  return (a >> 32) == 0ull ? (unsigned long long)((unsigned)a / b) : a / b;
-}
 // floor(U c / n), c <= n <= 2^15
-__device__ __forceinline__ unsigned long long units_before(unsigned long long U, unsigned c, unsigned n) {
-  const unsigned long long q = div64(U, n);
-  return q * c + (unsigned)(U - q * n) * c / n;
+__device__ __forceinline__ unsigned units_before(unsigned U, unsigned c, unsigned n) {
+  const unsigned q = U / n;
+  return q * c + (U - q * n) * c / n;
 }
 // CTA that has unit u
-__device__ __forceinline__ unsigned cta_of(unsigned long long U, unsigned long long u, unsigned n) { return (unsigned)(((u + 1) * n - 1) / U); }
-template <int ROWS, int UG> __device__ __forceinline__ unsigned cta_count(unsigned long long U, unsigned grid) {
-  const unsigned long long n = (U + Work<ROWS, UG>::MIN_UNITS - 1) / Work<ROWS, UG>::MIN_UNITS;
-  return n < grid ? (unsigned)n : grid;
+__device__ __forceinline__ unsigned cta_of(unsigned U, unsigned u, unsigned n) { return (unsigned)((((unsigned long long)u + 1) * n - 1) / U); }
+template <int ROWS, int UG> __device__ __forceinline__ unsigned cta_count(unsigned U, unsigned grid) {
+  const unsigned n = U / Work<ROWS, UG>::MIN_UNITS + (U % Work<ROWS, UG>::MIN_UNITS != 0 ? 1 : 0);
+  return n < grid ? n : grid;
 }
 
 // A CTA's run of units, item by item; whole warps walk through it together.
@@ -73,7 +69,7 @@ struct Piece {
   bool begins, whole;                                 // the item's first unit is this CTA's; all of them are
 };
 template <int ROWS, int UG> struct Walk {
-  unsigned long long u, end;
+  unsigned u, end;
   Item near;                                          // items 0 .. 31: most launches have no more
   int entries, tiles;
   // false: nothing to do for this CTA
@@ -82,8 +78,8 @@ template <int ROWS, int UG> struct Walk {
     entries = A.rows.B * tiles;
     const unsigned Hk = (unsigned)A.c.n_kv_heads;
     near = item_of<ROWS, UG>(A, lane, tiles, G, tell);
-    unsigned long long U = (unsigned long long)(unsigned)near.span * Hk;
-    for (int j = 32; j < entries; j += 32) U += (unsigned long long)(unsigned)item_of<ROWS, UG>(A, j + lane, tiles, G, tell).span * Hk;
+    unsigned U = (unsigned)near.span * Hk;
+    for (int j = 32; j < entries; j += 32) U += (unsigned)item_of<ROWS, UG>(A, j + lane, tiles, G, tell).span * Hk;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) U += __shfl_xor_sync(0xffffffffu, U, o);
     if (U == 0) return false;
@@ -96,10 +92,10 @@ template <int ROWS, int UG> struct Walk {
   __device__ __forceinline__ bool next(const Kv4Attn &A, int G, int lane, Piece &p) {
     if (u >= end) return false;
     const unsigned Hk = (unsigned)A.c.n_kv_heads;
-    unsigned long long before = 0;
+    unsigned before = 0;
     for (int j = 0;; j += 32) {                       // (some item has unit u)
       const Item it = j == 0 ? near : item_of<ROWS, UG>(A, j + lane, tiles, G, false);
-      const unsigned long long units = (unsigned long long)(unsigned)it.span * Hk, upto = before + scan(units, lane);
+      const unsigned units = (unsigned)it.span * Hk, upto = before + scan(units, lane);
       const unsigned hit = __ballot_sync(0xffffffffu, upto > u);
       if (hit == 0u) {
         before = __shfl_sync(0xffffffffu, upto, 31);
@@ -113,10 +109,10 @@ template <int ROWS, int UG> struct Walk {
       p.ctx = __shfl_sync(0xffffffffu, it.ctx, at);
       p.kv = __shfl_sync(0xffffffffu, it.kv, at);
       const int span = __shfl_sync(0xffffffffu, it.span, at);
-      const unsigned long long in = u - __shfl_sync(0xffffffffu, upto - units, at);
-      p.hk = (int)div64(in, (unsigned)span);
-      const int from = (int)(in - (unsigned long long)(unsigned)p.hk * (unsigned)span);
-      const int to = (int)min((unsigned long long)span, (unsigned long long)from + (end - u));
+      const unsigned in = u - __shfl_sync(0xffffffffu, upto - units, at);
+      p.hk = (int)(in / (unsigned)span);
+      const int from = (int)(in - (unsigned)p.hk * (unsigned)span);
+      const int to = (int)min((unsigned)span, (unsigned)from + (end - u));
       u += (unsigned)(to - from);
       p.lo = max(0, from - Work<ROWS, UG>::START);
       p.hi = max(0, to - Work<ROWS, UG>::START);
@@ -192,19 +188,19 @@ __global__ void __launch_bounds__(JOIN_THREADS) kv4_join_kernel(const Kv4Attn A,
   const int lane = threadIdx.x & 31, G = A.n_heads / A.c.n_kv_heads, entries = A.rows.B * tiles;
   const unsigned Hk = (unsigned)A.c.n_kv_heads;
   const Item near = item_of<ROWS, UG>(A, lane, tiles, G, false);
-  unsigned long long U = (unsigned long long)(unsigned)near.span * Hk;
-  for (int j = 32; j < entries; j += 32) U += (unsigned long long)(unsigned)item_of<ROWS, UG>(A, j + lane, tiles, G, false).span * Hk;
+  unsigned U = (unsigned)near.span * Hk;
+  for (int j = 32; j < entries; j += 32) U += (unsigned)item_of<ROWS, UG>(A, j + lane, tiles, G, false).span * Hk;
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) U += __shfl_xor_sync(0xffffffffu, U, o);
   const unsigned n = cta_count<ROWS, UG>(U, gridDim.x), c0 = blockIdx.x;
   int e = 0, hk = 0, first = 0, count = 0;
   unsigned c1 = c0;
   if (c0 + 1 < n) {
-    const unsigned long long begin = units_before(U, c0, n), end = units_before(U, c0 + 1, n), u = end - 1;
-    unsigned long long before = 0;
+    const unsigned begin = units_before(U, c0, n), end = units_before(U, c0 + 1, n), u = end - 1;
+    unsigned before = 0;
     for (int j = 0;; j += 32) {                       // (some item has unit u)
       const Item it = j == 0 ? near : item_of<ROWS, UG>(A, j + lane, tiles, G, false);
-      const unsigned long long units = (unsigned long long)(unsigned)it.span * Hk, upto = before + scan(units, lane);
+      const unsigned units = (unsigned)it.span * Hk, upto = before + scan(units, lane);
       const unsigned hit = __ballot_sync(0xffffffffu, upto > u);
       if (hit == 0u) {
         before = __shfl_sync(0xffffffffu, upto, 31);
@@ -215,9 +211,9 @@ __global__ void __launch_bounds__(JOIN_THREADS) kv4_join_kernel(const Kv4Attn A,
       first = __shfl_sync(0xffffffffu, it.first, at);
       count = __shfl_sync(0xffffffffu, it.count, at);
       const int span = __shfl_sync(0xffffffffu, it.span, at);
-      const unsigned long long start = __shfl_sync(0xffffffffu, upto - units, at);
-      hk = (int)div64(u - start, (unsigned)span);
-      const unsigned long long u0 = start + (unsigned long long)(unsigned)hk * (unsigned)span, u1 = u0 + (unsigned)span;
+      const unsigned start = __shfl_sync(0xffffffffu, upto - units, at);
+      hk = (int)((u - start) / (unsigned)span);
+      const unsigned u0 = start + (unsigned)hk * (unsigned)span, u1 = u0 + (unsigned)span;
       if (u0 >= begin && u1 > end) c1 = cta_of(U, u1 - 1, n);
       break;
     }
