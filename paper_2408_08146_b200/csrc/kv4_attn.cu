@@ -23,8 +23,6 @@
 
 namespace koala {
 
-int kv4_attention_ctas(int num_sms, int nt);
-
 namespace {
 
 constexpr int WARPS = 4;
@@ -66,13 +64,15 @@ __device__ __forceinline__ uint4 lds128(uint32_t at) {
   return v;
 }
 
+// CTAs that share an SM, by registers: four warps hide too little of each other's waits with three (one sequence of 131071 slots MEASURE)
+template <int NT, bool PAIR> constexpr int CTAS = NT == 1 ? (PAIR ? 3 : 4) : 2;
 template <int NT> constexpr int DEPTH = NT == 1 ? 3 : 5;      // steps of a warp in its ring
 // Granules per step of a warp: two where registers allow, for independent instructions and half the bookkeeping.
 template <int NT> constexpr int STEP = NT == 1 ? 2 : 1;
 template <int DH, int NT> constexpr int RING = WARPS * DEPTH<NT> * STEP<NT> * kv4_granule_bytes(DH);
 
 template <int DH, int NT, bool PAIR>
-__global__ void __launch_bounds__(32 * WARPS, NT == 1 ? 3 : 2) kv4_attn_kernel(const Kv4Attn A, float *__restrict__ scratch, int tiles) {
+__global__ void __launch_bounds__(32 * WARPS, CTAS<NT, PAIR>) kv4_attn_kernel(const Kv4Attn A, float *__restrict__ scratch, int tiles) {
   constexpr int KS = DH / 16;              // depth steps of S
   constexpr int MT = DH / 16;              // tiles of 16 dims of O
   constexpr int ROWS = 8 * NT, OS = DH + 4, GB = kv4_granule_bytes(DH), H = STEP<NT>, STAGES = DEPTH<NT>;
@@ -494,20 +494,19 @@ template <int DH, int NT, bool PAIR> cudaError_t go(Launch L, const Kv4Attn &a, 
   cudaError_t e = optin.ensure((const void *)kv4_attn_kernel<DH, NT, PAIR>, RING<DH, NT>);
   if (e != cudaSuccess) return e;
   const int G = a.n_heads / a.c.n_kv_heads, rows = a.rows.max_rows * G, tiles = (rows + 8 * NT - 1) / (8 * NT);
-  const int grid = kv4_attention_ctas(num_sms, NT);
+  const int grid = num_sms * CTAS<NT, PAIR>;
   e = launch_k(kv4_attn_kernel<DH, NT, PAIR>, dim3(grid), dim3(32 * WARPS), RING<DH, NT>, L.st, L.pdl, a, a.scratch, tiles);
   if (e != cudaSuccess) return e;
-  return launch_k(kv4_join_kernel<DH, 8 * NT, 1>, dim3(grid), dim3(JOIN_THREADS), 0, L.st, L.pdl, a, a.scratch, tiles);
+  return join<DH, 8 * NT, 1>(L, a, grid, tiles, rows, num_sms);
 }
 
 }  // namespace
 
-int kv4_attention_ctas(int num_sms, int nt) { return num_sms * (nt == 1 ? 3 : 2); }
 
 size_t kv4_attention_scratch(int dh, int num_sms, int rows) {
   if (rows > KV4_FEW_ROWS) return kv4_attention_tc_scratch(dh, num_sms);
   const int nt = rows > 8 ? 2 : 1;
-  return (size_t)kv4_attention_ctas(num_sms, nt) * 2 * (8 * nt) * (dh + 4) * sizeof(float);
+  return (size_t)num_sms * (nt == 1 ? CTAS<1, false> : CTAS<2, false>) * 2 * (8 * nt) * (dh + 4) * sizeof(float);
 }
 
 cudaError_t kv4_attention(Launch L, int dh, const Kv4Attn &args, int num_sms) {

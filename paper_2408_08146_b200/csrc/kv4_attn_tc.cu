@@ -807,8 +807,7 @@ template <int DH, int MODE> cudaError_t go(Launch L, const Kv4Attn &a, int num_s
   const int rows = a.rows.max_rows * (a.n_heads / a.c.n_kv_heads), tiles = (rows + ROWS - 1) / ROWS;
   e = launch_k(kv4_attn_tc_kernel<DH, MODE>, dim3(num_sms), dim3(THREADS), SMEM<DH>, L.st, L.pdl, a, a.scratch, tiles);
   if (e != cudaSuccess) return e;
-  const int in_tile = rows < ROWS ? rows : ROWS;
-  return launch_k(kv4_join_kernel<DH, ROWS, UG>, dim3(num_sms, (in_tile + JOIN_ROWS - 1) / JOIN_ROWS), dim3(JOIN_THREADS), 0, L.st, L.pdl, a, a.scratch, tiles);
+  return join<DH, ROWS, UG>(L, a, num_sms, tiles, rows, num_sms);
 }
 
 }  // namespace

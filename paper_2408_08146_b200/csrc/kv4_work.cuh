@@ -70,16 +70,14 @@ struct Piece {
 };
 template <int ROWS, int UG> struct Walk {
   unsigned u, end;
-  Item near;                                          // items 0 .. 31: most launches have no more
   int entries, tiles;
   // false: nothing to do for this CTA
   __device__ __forceinline__ bool begin(const Kv4Attn &A, int n_tiles, int G, int lane, bool tell) {
     tiles = n_tiles;
     entries = A.rows.B * tiles;
     const unsigned Hk = (unsigned)A.c.n_kv_heads;
-    near = item_of<ROWS, UG>(A, lane, tiles, G, tell);
-    unsigned U = (unsigned)near.span * Hk;
-    for (int j = 32; j < entries; j += 32) U += (unsigned)item_of<ROWS, UG>(A, j + lane, tiles, G, tell).span * Hk;
+    unsigned U = 0;
+    for (int j = 0; j < entries; j += 32) U += (unsigned)item_of<ROWS, UG>(A, j + lane, tiles, G, tell).span * Hk;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) U += __shfl_xor_sync(0xffffffffu, U, o);
     if (U == 0) return false;
@@ -94,7 +92,7 @@ template <int ROWS, int UG> struct Walk {
     const unsigned Hk = (unsigned)A.c.n_kv_heads;
     unsigned before = 0;
     for (int j = 0;; j += 32) {                       // (some item has unit u)
-      const Item it = j == 0 ? near : item_of<ROWS, UG>(A, j + lane, tiles, G, false);
+      const Item it = item_of<ROWS, UG>(A, j + lane, tiles, G, false);
       const unsigned units = (unsigned)it.span * Hk, upto = before + scan(units, lane);
       const unsigned hit = __ballot_sync(0xffffffffu, upto > u);
       if (hit == 0u) {
@@ -175,31 +173,53 @@ __device__ __forceinline__ void finish(const Kv4Attn &A, int first, int hk, int 
   store_out(A, at, v);
 }
 
-// Joins the parts of the item that begins in CTA blockIdx.x of the launch before and goes on behind it (there is at most one: a block for each CTA, not for
-// each item, is few blocks whatever the launch).  grid (CTAs, blocks of JOIN_ROWS rows): for each row as many groups of DH / 4 threads
-// as there are, which take its parts in turn, BATCH at a time on their way together.
-constexpr int JOIN_ROWS = 16, JOIN_THREADS = 512;
+// Joins the parts of the items that lie in several CTAs.  grid (items, blocks of `per` rows), or, where there are more items than CTAs, (CTAs, ..): the one
+// item that begins in that CTA and goes on behind it.  A block takes 3 us even when it finds nothing to do, so few of them, two a SM
+// at most where the rows allow.  For each row as many groups of DH / 4 threads as there are, which take its parts in turn, BATCH at a time
+// on their way together.
+constexpr int JOIN_THREADS = 512;
 template <int DH, int ROWS, int UG>
-__global__ void __launch_bounds__(JOIN_THREADS) kv4_join_kernel(const Kv4Attn A, float *scratch, int tiles) {
+__global__ void __launch_bounds__(JOIN_THREADS) kv4_join_kernel(const Kv4Attn A, float *scratch, int tiles, int per, unsigned ctas, int by_item) {
   constexpr int LANES = DH / 4, SLOTS = JOIN_THREADS / LANES, BATCH = 5;
   __shared__ float4 acc[SLOTS][LANES];
   __shared__ float2 ml[SLOTS];
   pdl_launch_dependents();
   const int lane = threadIdx.x & 31, G = A.n_heads / A.c.n_kv_heads, entries = A.rows.B * tiles;
   const unsigned Hk = (unsigned)A.c.n_kv_heads;
-  const Item near = item_of<ROWS, UG>(A, lane, tiles, G, false);
-  unsigned U = (unsigned)near.span * Hk;
-  for (int j = 32; j < entries; j += 32) U += (unsigned)item_of<ROWS, UG>(A, j + lane, tiles, G, false).span * Hk;
+  int e = by_item ? (int)(blockIdx.x / Hk) : 0, hk = by_item ? (int)(blockIdx.x % Hk) : 0, first = 0, count = 0, span = 0;
+  unsigned U = 0, start = 0;               // all units; those before entry e
+  for (int j = 0; j < entries; j += 32) {
+    const Item it = item_of<ROWS, UG>(A, j + lane, tiles, G, false);
+    const unsigned units = (unsigned)it.span * Hk;
+    U += units;
+    if (by_item) {
+      start += j + lane < e ? units : 0u;
+      if (e >= j && e < j + 32) {
+        first = __shfl_sync(0xffffffffu, it.first, e - j);
+        count = __shfl_sync(0xffffffffu, it.count, e - j);
+        span = __shfl_sync(0xffffffffu, it.span, e - j);
+      }
+    }
+  }
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) U += __shfl_xor_sync(0xffffffffu, U, o);
-  const unsigned n = cta_count<ROWS, UG>(U, gridDim.x), c0 = blockIdx.x;
-  int e = 0, hk = 0, first = 0, count = 0;
-  unsigned c1 = c0;
-  if (c0 + 1 < n) {
+  for (int o = 16; o > 0; o >>= 1) {
+    U += __shfl_xor_sync(0xffffffffu, U, o);
+    start += __shfl_xor_sync(0xffffffffu, start, o);
+  }
+  const unsigned n = cta_count<ROWS, UG>(U, ctas);
+  unsigned c0 = blockIdx.x, c1 = c0;
+  if (by_item) {
+    c0 = c1 = 0;
+    if (span > 0) {
+      const unsigned u0 = start + (unsigned)hk * (unsigned)span;
+      c0 = cta_of(U, u0, n);
+      c1 = cta_of(U, u0 + (unsigned)span - 1, n);
+    }
+  } else if (c0 + 1 < n) {
     const unsigned begin = units_before(U, c0, n), end = units_before(U, c0 + 1, n), u = end - 1;
     unsigned before = 0;
     for (int j = 0;; j += 32) {                       // (some item has unit u)
-      const Item it = j == 0 ? near : item_of<ROWS, UG>(A, j + lane, tiles, G, false);
+      const Item it = item_of<ROWS, UG>(A, j + lane, tiles, G, false);
       const unsigned units = (unsigned)it.span * Hk, upto = before + scan(units, lane);
       const unsigned hit = __ballot_sync(0xffffffffu, upto > u);
       if (hit == 0u) {
@@ -210,8 +230,8 @@ __global__ void __launch_bounds__(JOIN_THREADS) kv4_join_kernel(const Kv4Attn A,
       e = j + at;
       first = __shfl_sync(0xffffffffu, it.first, at);
       count = __shfl_sync(0xffffffffu, it.count, at);
-      const int span = __shfl_sync(0xffffffffu, it.span, at);
-      const unsigned start = __shfl_sync(0xffffffffu, upto - units, at);
+      span = __shfl_sync(0xffffffffu, it.span, at);
+      start = __shfl_sync(0xffffffffu, upto - units, at);
       hk = (int)((u - start) / (unsigned)span);
       const unsigned u0 = start + (unsigned)hk * (unsigned)span, u1 = u0 + (unsigned)span;
       if (u0 >= begin && u1 > end) c1 = cta_of(U, u1 - 1, n);
@@ -219,8 +239,8 @@ __global__ void __launch_bounds__(JOIN_THREADS) kv4_join_kernel(const Kv4Attn A,
     }
   }
   pdl_wait();                              // by every block, whatever it has to do: the launch must not end before the one it joins
-  const int row0 = (tiles == 1 ? 0 : e % tiles) * ROWS + blockIdx.y * JOIN_ROWS;
-  const int rows = min(JOIN_ROWS, count * G - row0);
+  const int tile0 = (tiles == 1 ? 0 : e % tiles) * ROWS, row0 = tile0 + blockIdx.y * per;
+  const int rows = min(per, min(ROWS, count * G - tile0) - (int)blockIdx.y * per);
   if (c1 == c0 || rows <= 0) return;
   int r2 = 1;
   while (r2 < rows) r2 *= 2;
@@ -236,7 +256,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) kv4_join_kernel(const Kv4Attn A,
       const unsigned ck = c + k * groups;
       q[k] = make_float2(-INFINITY, 0.f);
       if (ck > c1) continue;
-      const float *p = part_of<DH, ROWS>(scratch, ck, ck == c0) + (blockIdx.y * JOIN_ROWS + r) * PART_ROW<DH>;
+      const float *p = part_of<DH, ROWS>(scratch, ck, ck == c0) + (blockIdx.y * per + r) * PART_ROW<DH>;
       q[k] = *reinterpret_cast<const float2 *>(p + DH);
       x[k] = *reinterpret_cast<const float4 *>(p + 4 * l);
     }
@@ -271,6 +291,17 @@ __global__ void __launch_bounds__(JOIN_THREADS) kv4_join_kernel(const Kv4Attn A,
     }
   }
   if (in) finish(A, first, hk, G, row0 + r, 4 * l, v, sum);
+}
+
+// rows: of one sequence and kv head
+template <int DH, int ROWS, int UG> cudaError_t join(Launch L, const Kv4Attn &a, int ctas, int tiles, int rows, int num_sms) {
+  const int in_tile = rows < ROWS ? rows : ROWS;
+  const long long items = (long long)a.rows.B * tiles * a.c.n_kv_heads;
+  const int by_item = items <= ctas ? 1 : 0, gx = by_item ? (int)items : ctas;
+  int per = (int)(((long long)in_tile * gx + 2 * num_sms - 1) / (2 * num_sms));
+  per = per < 1 ? 1 : per > 16 ? 16 : per;
+  return launch_k(kv4_join_kernel<DH, ROWS, UG>, dim3(gx, (in_tile + per - 1) / per), dim3(JOIN_THREADS), 0, L.st, L.pdl, a, a.scratch, tiles, per, (unsigned)ctas,
+                  by_item);
 }
 
 }  // namespace
