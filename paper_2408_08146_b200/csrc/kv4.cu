@@ -29,11 +29,12 @@ template <typename T> __device__ __forceinline__ void store4(T *p, const float *
 
 // Where the new rows come from: the caller's tensors, or the partial sums of the Q/K/V multiply.
 template <typename T> struct FromTensors {
-  Kv4Tensor x[3];      // q, k, v
+  Kv4Tensor q, k, v;
   __device__ __forceinline__ void load(int which, int r, int h, int c, float *a) const {
-    load4(reinterpret_cast<const T *>(x[which].p) + (long long)r * x[which].row + (long long)h * x[which].head + c, a);
+    const void *p = which == 0 ? q.p : which == 1 ? k.p : v.p;
+    const long long row = which == 0 ? q.row : which == 1 ? k.row : v.row, head = which == 0 ? q.head : which == 1 ? k.head : v.head;
+    load4(reinterpret_cast<const T *>(p) + (long long)r * row + (long long)h * head + c, a);
   }
-  __device__ __forceinline__ float scale(int) const { return 1.f; }
 };
 
 // One vector of a row: DH / 8 lanes, lane l with dims 4l .. 4l+3 (a) and DH/2 + 4l .. (b).
@@ -84,119 +85,156 @@ template <int DH> __device__ __forceinline__ uint32_t quantise(const float *a, c
   return w;
 }
 
-// grid (rows, groups of vectors): a block takes 256 * 8 / DH of the row's n_q + 2 n_kv vectors.
-template <int DH, typename Src, typename TQ>
+// Rows of a block: their places are looked up by a lane each, which takes four dependent loads (3 us of the 3.6 us that a block with one
+// row takes), and the loads of ROWS_AT_ONCE rows are on their way together.  One row where that leaves SMs without a block.
+constexpr int BLOCK_ROWS = 16, ROWS_AT_ONCE = 4;
+
+// grid (blocks of rows, groups of vectors): a block takes 256 * 8 / DH of the rows' n_q + 2 n_kv vectors.
+// Bound: bytes (append_prompt MEASURE).  MANY: BLOCK_ROWS rows a block, else one.
+template <int DH, bool MANY, typename Src, typename TQ>
 __global__ void __launch_bounds__(256) kv4_append_kernel(Kv4Cache c, size_t layer_off, Kv4Rows rows, Src src, int n_q, Kv4Tensor q_out,
                                                          const float *rope, const int32_t *pos, int n_pos) {
-  constexpr int LPV = DH / 8;
+  constexpr int LPV = DH / 8, RB = MANY ? BLOCK_ROWS : 1, AT = MANY ? ROWS_AT_ONCE : 1;
   pdl_launch_dependents();
   pdl_wait();
-  const int r = blockIdx.x, lane = threadIdx.x & 31;
-  const int vec = blockIdx.y * (256 / LPV) + threadIdx.x / LPV, l = threadIdx.x % LPV;
-  const int n_vec = n_q + 2 * c.n_kv_heads;
   rows.check();
-  const int b = rows.sequence_of(r, lane);
-  if (b < 0) return;
-  int first, count;
-  rows.range(b, first, count);
-  const int i = r - first;
-  if (i >= count) return;
-  const int slot = rows.slot != nullptr ? rows.slot[r] : rows.ctx_len[b] + i;
-  if (slot < 0) {
-    if (rows.slot == nullptr) rows.report();
-    return;
-  }
-  const int p = pos != nullptr ? pos[r] : slot;
-  if (rope != nullptr && (unsigned)p >= (unsigned)n_pos) { rows.report(); return; }
-  const int page = c.page_of(rows.cache_of(b), slot >> 4);
-  if ((unsigned)page >= (unsigned)c.n_pages) { rows.report(); return; }
-  bool shadowed = false;        // a later row of the sequence has the same slot: that one is kept
-  if (rows.slot != nullptr)
-    for (int j = i + 1 + lane; j < count; j += 32) shadowed = shadowed || rows.slot[first + j] == slot;
-  shadowed = __any_sync(0xffffffffu, shadowed);
+  const int lane = threadIdx.x & 31, r0 = blockIdx.x * RB;
+  const int vec = blockIdx.y * (256 / LPV) + threadIdx.x / LPV, l = threadIdx.x % LPV;
+  const bool live = vec < n_q + 2 * c.n_kv_heads;
   const int which = vec < n_q ? 0 : vec < n_q + c.n_kv_heads ? 1 : 2;
   const int h = which == 0 ? vec : which == 1 ? vec - n_q : vec - n_q - c.n_kv_heads;
-  float a[4] = {0.f, 0.f, 0.f, 0.f}, e[4] = {0.f, 0.f, 0.f, 0.f};
-  const bool live = vec < n_vec;
-  if (live) {
-    src.load(which, r, h, 4 * l, a);
-    src.load(which, r, h, DH / 2 + 4 * l, e);
+  // lane j: row r0 + j
+  Kv4Place mine{-1, -1, 0, 0, 0};
+  int turn = 0;
+  if (lane < RB) {
+    mine = kv4_place(c, rows, r0 + lane);
+    turn = pos != nullptr && mine.page >= 0 ? pos[r0 + lane] : mine.slot;
+    if (mine.page >= 0 && rope != nullptr && (unsigned)turn >= (unsigned)n_pos) {
+      rows.report();
+      mine.page = -1;
+    }
   }
-  if (rope != nullptr && which < 2) {
-    float cs[8];
-    const float4 *t = reinterpret_cast<const float4 *>(rope + ((size_t)p * (DH / 2) + 4 * l) * 2);
-    *reinterpret_cast<float4 *>(cs) = t[0];
-    *reinterpret_cast<float4 *>(cs + 4) = t[1];
-    rotate4(a, e, cs);
-  }
-  if (live && which == 0) {
-    TQ *o = reinterpret_cast<TQ *>(q_out.p) + (long long)r * q_out.row + (long long)h * q_out.head + 4 * l;
-    store4(o, a);
-    store4(o + DH / 2, e);
-  }
-  uint32_t params;
-  const uint32_t w = quantise<DH>(a, e, params);          // (whole warps: the vectors of a warp may be of both kinds)
-  if (live && which != 0 && !shadowed) {
-    unsigned char *g = c.pages + layer_off + c.granule<DH>(page, h, slot >> 4);
-    const int s = slot & 15;
-    *reinterpret_cast<uint32_t *>(g + (which == 1 ? kv4_k_at<DH>(s, l) : kv4_v_at<DH>(s, l))) = w;
-    if (l == 0) *reinterpret_cast<uint32_t *>(g + kv4_p_at<DH>(s, which - 1)) = params;
+  unsigned shadowed = 0u;       // bit j: a later row of the sequence has row j's slot: that one is kept
+  if (rows.slot != nullptr)
+    for (int j = 0; j < RB; ++j) {
+      const int slot = __shfl_sync(0xffffffffu, mine.slot, j), first = __shfl_sync(0xffffffffu, mine.first, j);
+      const int i = __shfl_sync(0xffffffffu, mine.i, j), count = __shfl_sync(0xffffffffu, mine.count, j);
+      bool again = false;
+      for (int k = i + 1 + lane; k < count; k += 32) again = again || rows.slot[first + k] == slot;
+      if (__any_sync(0xffffffffu, again)) shadowed |= 1u << j;
+    }
+  const bool any_kv = __any_sync(0xffffffffu, which != 0);       // warps of nothing but queries have nothing to quantise
+  unsigned char *base = c.pages + layer_off;
+#pragma unroll 1
+  for (int j0 = 0; j0 < RB; j0 += AT) {
+    float a[AT][4], e[AT][4];
+    float4 cs[AT][2];
+    int page[AT], slot[AT];
+#pragma unroll
+    for (int k = 0; k < AT; ++k) {
+      page[k] = __shfl_sync(0xffffffffu, mine.page, j0 + k);
+      slot[k] = __shfl_sync(0xffffffffu, mine.slot, j0 + k);
+      const int p = __shfl_sync(0xffffffffu, turn, j0 + k);
+      const bool use = live && page[k] >= 0;
+#pragma unroll
+      for (int x = 0; x < 4; ++x) a[k][x] = e[k][x] = 0.f;
+      if (use) {
+        src.load(which, r0 + j0 + k, h, 4 * l, a[k]);
+        src.load(which, r0 + j0 + k, h, DH / 2 + 4 * l, e[k]);
+      }
+      if (rope != nullptr && use && which < 2) {
+        const float4 *t = reinterpret_cast<const float4 *>(rope + ((size_t)p * (DH / 2) + 4 * l) * 2);
+        cs[k][0] = t[0];
+        cs[k][1] = t[1];
+      } else {
+        cs[k][0] = cs[k][1] = make_float4(1.f, 0.f, 1.f, 0.f);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < AT; ++k) {
+      if (page[k] < 0) continue;           // (the same for the whole block)
+      const int r = r0 + j0 + k;
+      if (rope != nullptr && which < 2) rotate4(a[k], e[k], &cs[k][0].x);
+      if (live && which == 0) {
+        TQ *o = reinterpret_cast<TQ *>(q_out.p) + (long long)r * q_out.row + (long long)h * q_out.head + 4 * l;
+        store4(o, a[k]);
+        store4(o + DH / 2, e[k]);
+      }
+      if (!any_kv) continue;
+      uint32_t params;
+      const uint32_t w = quantise<DH>(a[k], e[k], params);       // (whole warps: the vectors of a warp may be of both kinds)
+      if (live && which != 0 && (shadowed >> (j0 + k) & 1u) == 0u) {
+        unsigned char *g = base + c.granule<DH>(page[k], h, slot[k] >> 4);
+        const int s = slot[k] & 15;
+        *reinterpret_cast<uint32_t *>(g + (which == 1 ? kv4_k_at<DH>(s, l) : kv4_v_at<DH>(s, l))) = w;
+        if (l == 0) *reinterpret_cast<uint32_t *>(g + kv4_p_at<DH>(s, which - 1)) = params;
+      }
+    }
   }
 }
 
-// grid (rows, groups of vectors, layers)
-template <int DH, typename T>
+// grid (blocks of rows, groups of vectors, layers)
+template <int DH, bool MANY, typename T>
 __global__ void __launch_bounds__(256) kv4_read_kernel(Kv4Cache c, int layer0, Kv4Rows rows, Kv4Tensor k_out, Kv4Tensor v_out, long long k_layer,
                                                        long long v_layer) {
-  constexpr int LPV = DH / 8;
+  constexpr int LPV = DH / 8, RB = MANY ? BLOCK_ROWS : 1, AT = MANY ? 2 * ROWS_AT_ONCE : 1;
   pdl_launch_dependents();
   pdl_wait();
-  const int r = blockIdx.x, lane = threadIdx.x & 31;
-  const int vec = blockIdx.y * (256 / LPV) + threadIdx.x / LPV, l = threadIdx.x % LPV;
   rows.check();
-  const int b = rows.sequence_of(r, lane);
-  if (b < 0) return;
-  int first, count;
-  rows.range(b, first, count);
-  const int i = r - first;
-  if (i >= count || vec >= 2 * c.n_kv_heads) return;
-  const int slot = rows.slot != nullptr ? rows.slot[r] : rows.ctx_len[b] + i;
-  const int page = slot < 0 ? -1 : c.page_of(rows.cache_of(b), slot >> 4);
-  if ((unsigned)page >= (unsigned)c.n_pages) {
-    if (slot >= 0 || rows.slot == nullptr) rows.report();
-    return;
-  }
-  const int is_v = vec >= c.n_kv_heads, h = is_v ? vec - c.n_kv_heads : vec, s = slot & 15;
-  const unsigned char *g = c.pages + (size_t)(layer0 + blockIdx.z) * c.layer_bytes + c.granule<DH>(page, h, slot >> 4);
-  const uint32_t w = *reinterpret_cast<const uint32_t *>(g + (is_v ? kv4_v_at<DH>(s, l) : kv4_k_at<DH>(s, l)));
-  const uint32_t params = *reinterpret_cast<const uint32_t *>(g + kv4_p_at<DH>(s, is_v));
-  const float scale = __uint_as_float(params << 16), zero = __uint_as_float(params & 0xffff0000u);
-  float a[4], e[4];
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {          // scale * code is exact in fp32
-    a[k] = zero + scale * (float)((w >> (4 * k)) & 15u);
-    e[k] = zero + scale * (float)((w >> (16 + 4 * k)) & 15u);
-  }
+  const int lane = threadIdx.x & 31, r0 = blockIdx.x * RB;
+  const int vec = blockIdx.y * (256 / LPV) + threadIdx.x / LPV, l = threadIdx.x % LPV;
+  const int is_v = vec >= c.n_kv_heads, h = is_v ? vec - c.n_kv_heads : vec;
+  Kv4Place mine{-1, -1, 0, 0, 0};
+  if (lane < RB) mine = kv4_place(c, rows, r0 + lane);
   const Kv4Tensor &t = is_v ? v_out : k_out;
-  if (t.p == nullptr) return;
-  T *o = reinterpret_cast<T *>(t.p) + (long long)blockIdx.z * (is_v ? v_layer : k_layer) + (long long)r * t.row + (long long)h * t.head + 4 * l;
-  store4(o, a);
-  store4(o + DH / 2, e);
+  const bool live = vec < 2 * c.n_kv_heads && t.p != nullptr;
+  const unsigned char *base = c.pages + (size_t)(layer0 + blockIdx.z) * c.layer_bytes;
+  T *out = reinterpret_cast<T *>(t.p) + (long long)blockIdx.z * (is_v ? v_layer : k_layer) + (long long)h * t.head + 4 * l;
+#pragma unroll 1
+  for (int j0 = 0; j0 < RB; j0 += AT) {
+    uint32_t w[AT], params[AT];
+    int page[AT];
+#pragma unroll
+    for (int k = 0; k < AT; ++k) {
+      page[k] = __shfl_sync(0xffffffffu, mine.page, j0 + k);
+      const int slot = __shfl_sync(0xffffffffu, mine.slot, j0 + k), s = slot & 15;
+      w[k] = params[k] = 0u;
+      if (!live || page[k] < 0) continue;
+      const unsigned char *g = base + c.granule<DH>(page[k], h, slot >> 4);
+      w[k] = *reinterpret_cast<const uint32_t *>(g + (is_v ? kv4_v_at<DH>(s, l) : kv4_k_at<DH>(s, l)));
+      params[k] = *reinterpret_cast<const uint32_t *>(g + kv4_p_at<DH>(s, is_v));
+    }
+#pragma unroll
+    for (int k = 0; k < AT; ++k) {
+      if (!live || page[k] < 0) continue;
+      const float scale = __uint_as_float(params[k] << 16), zero = __uint_as_float(params[k] & 0xffff0000u);
+      float a[4], e[4];
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {        // scale * code is exact in fp32
+        a[x] = zero + scale * (float)((w[k] >> (4 * x)) & 15u);
+        e[x] = zero + scale * (float)((w[k] >> (16 + 4 * x)) & 15u);
+      }
+      T *o = out + (long long)(r0 + j0 + k) * t.row;
+      store4(o, a);
+      store4(o + DH / 2, e);
+    }
+  }
 }
 
-// grid (kv heads, sequences, layers): slot dst[i] <- slot src[i], i < n, all reads before all writes.
-template <int DH>
-__global__ void __launch_bounds__(128) kv4_move_kernel(Kv4Cache c, Kv4Moves m) {
+// Slot dst[i] <- slot src[i], i < n, all reads before all writes.  grid (blocks of (layer, kv head) pairs, sequences); a warp takes a pair at a time.
+// The words of a pair's slots wait in registers where they fit (SMALL: n (DH / 4 + 2) <= 32 HELD), else in shared memory.
+constexpr int MOVE_WARPS = 8, HELD = 12;
+template <int DH, bool SMALL>
+__global__ void __launch_bounds__(32 * MOVE_WARPS) kv4_move_kernel(Kv4Cache c, Kv4Moves m, int pairs_per_block) {
   constexpr int LPV = DH / 8, NW = 2 * LPV + 2;         // words of a slot: codes of K and of V, two words of parameters
-  __shared__ long long from[KV4_MAX_MOVES], to[KV4_MAX_MOVES];
+  __shared__ long long from[KV4_MAX_MOVES], to[KV4_MAX_MOVES];      // granules of kv head 0
   __shared__ int in_granule[KV4_MAX_MOVES];             // slots inside their granules: source | destination << 8
   __shared__ int dst_slot[KV4_MAX_MOVES];
-  extern __shared__ uint32_t words[];                   // [n][NW]
+  extern __shared__ uint32_t words[];                   // [n][NW] of a warp
   pdl_launch_dependents();
   pdl_wait();
-  const int h = blockIdx.x, b = blockIdx.y;
+  const int b = blockIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int n = min(m.count != nullptr ? m.count[b] : m.n, m.n);
-  unsigned char *base = c.pages + (size_t)blockIdx.z * c.layer_bytes;
   const int S = m.base != nullptr ? m.base[b] : 0;
   for (int i = threadIdx.x; i < n; i += blockDim.x) {
     int src = m.src[(size_t)b * m.stride + i], dst = m.dst != nullptr ? m.dst[(size_t)b * m.stride + i] : i;
@@ -204,8 +242,8 @@ __global__ void __launch_bounds__(128) kv4_move_kernel(Kv4Cache c, Kv4Moves m) {
     if (used) { src += S; dst += S; }
     long long f = -1, t = -1;
     if (used && src != dst) {
-      f = c.granule<DH>(c.page_of(b, src >> 4), h, src >> 4);
-      t = c.granule<DH>(c.page_of(b, dst >> 4), h, dst >> 4);
+      f = c.granule<DH>(c.page_of(b, src >> 4), 0, src >> 4);
+      t = c.granule<DH>(c.page_of(b, dst >> 4), 0, dst >> 4);
       if (f < 0 || t < 0) {
         if (m.status != nullptr) atomicMax(m.status, 1);
         f = t = -1;
@@ -217,35 +255,86 @@ __global__ void __launch_bounds__(128) kv4_move_kernel(Kv4Cache c, Kv4Moves m) {
     dst_slot[i] = used ? dst : -1;
   }
   __syncthreads();
-  auto at = [&](int s, int w) { return w < LPV ? kv4_k_at<DH>(s, w) : w < 2 * LPV ? kv4_v_at<DH>(s, w - LPV) : kv4_p_at<DH>(s, w - 2 * LPV); };
-  for (int e = threadIdx.x; e < n * NW; e += blockDim.x) {
-    const int i = e / NW, w = e - i * NW;
-    if (from[i] >= 0) words[e] = *reinterpret_cast<const uint32_t *>(base + from[i] + at(in_granule[i] & 15, w));
-  }
   // of moves to the same slot the last one is kept
   for (int i = threadIdx.x; i < n; i += blockDim.x)
     for (int j = i + 1; j < n; ++j)
       if (dst_slot[i] >= 0 && dst_slot[j] == dst_slot[i]) to[i] = -1;
   __syncthreads();
-  for (int e = threadIdx.x; e < n * NW; e += blockDim.x) {
-    const int i = e / NW, w = e - i * NW;
-    if (from[i] >= 0 && to[i] >= 0) *reinterpret_cast<uint32_t *>(base + to[i] + at(in_granule[i] >> 8, w)) = words[e];
+  auto at = [&](int s, int w) { return w < LPV ? kv4_k_at<DH>(s, w) : w < 2 * LPV ? kv4_v_at<DH>(s, w - LPV) : kv4_p_at<DH>(s, w - 2 * LPV); };
+  const long long head_bytes = (long long)kv4_granule_bytes(DH) << c.gpp_shift;
+  const int pairs = c.n_layers * c.n_kv_heads, end = min(pairs, (int)(blockIdx.x + 1) * pairs_per_block);
+  if constexpr (SMALL) {
+    long long f[HELD], t[HELD];
+#pragma unroll
+    for (int k = 0; k < HELD; ++k) {
+      const int e = lane + 32 * k, i = e / NW, w = e - i * NW;
+      f[k] = t[k] = -1;
+      if (e < n * NW && from[i] >= 0 && to[i] >= 0) {
+        f[k] = from[i] + at(in_granule[i] & 15, w);
+        t[k] = to[i] + at(in_granule[i] >> 8, w);
+      }
+    }
+    for (int p = blockIdx.x * pairs_per_block + warp; p < end; p += MOVE_WARPS) {
+      unsigned char *base = c.pages + (size_t)(p / c.n_kv_heads) * c.layer_bytes + (p % c.n_kv_heads) * head_bytes;
+      uint32_t held[HELD];
+#pragma unroll
+      for (int k = 0; k < HELD; ++k) held[k] = f[k] >= 0 ? *reinterpret_cast<const uint32_t *>(base + f[k]) : 0u;
+      __syncwarp();                        // every lane has read
+#pragma unroll
+      for (int k = 0; k < HELD; ++k)
+        if (t[k] >= 0) *reinterpret_cast<uint32_t *>(base + t[k]) = held[k];
+      __syncwarp();
+    }
+  } else {
+    for (int p = blockIdx.x * pairs_per_block; p < end; ++p) {
+      unsigned char *base = c.pages + (size_t)(p / c.n_kv_heads) * c.layer_bytes + (p % c.n_kv_heads) * head_bytes;
+      for (int e = threadIdx.x; e < n * NW; e += blockDim.x) {
+        const int i = e / NW, w = e - i * NW;
+        if (from[i] >= 0) words[e] = *reinterpret_cast<const uint32_t *>(base + from[i] + at(in_granule[i] & 15, w));
+      }
+      __syncthreads();
+      for (int e = threadIdx.x; e < n * NW; e += blockDim.x) {
+        const int i = e / NW, w = e - i * NW;
+        if (from[i] >= 0 && to[i] >= 0) *reinterpret_cast<uint32_t *>(base + to[i] + at(in_granule[i] >> 8, w)) = words[e];
+      }
+      __syncthreads();
+    }
   }
 }
+
+constexpr int NUM_SMS = 148;
+// BLOCK_ROWS rows a block only where that still gives every SM a block
+bool many_rows(int total, int slices) { return (long long)((total + BLOCK_ROWS - 1) / BLOCK_ROWS) * slices >= 2 * NUM_SMS; }
 
 template <int DH, typename T>
 cudaError_t append_t(Launch L, const Kv4Cache &c, size_t layer_off, const Kv4Rows &rows, const Kv4Tensor *x, int n_q, Kv4Tensor q_out, const float *rope,
                      const int32_t *pos, int n_pos) {
   const int per = 256 * 8 / DH, n_vec = n_q + 2 * c.n_kv_heads;
-  const FromTensors<T> src{{x[0], x[1], x[2]}};
-  return launch_k(kv4_append_kernel<DH, FromTensors<T>, T>, dim3(rows.total, (n_vec + per - 1) / per), dim3(256), 0, L.st, L.pdl, c, layer_off, rows,
-                  src, n_q, q_out, rope, pos, n_pos);
+  const FromTensors<T> src{x[0], x[1], x[2]};
+  const int slices = (n_vec + per - 1) / per;
+  if (many_rows(rows.total, slices))
+    return launch_k(kv4_append_kernel<DH, true, FromTensors<T>, T>, dim3((rows.total + BLOCK_ROWS - 1) / BLOCK_ROWS, slices), dim3(256), 0, L.st, L.pdl, c,
+                    layer_off, rows, src, n_q, q_out, rope, pos, n_pos);
+  return launch_k(kv4_append_kernel<DH, false, FromTensors<T>, T>, dim3(rows.total, slices), dim3(256), 0, L.st, L.pdl, c, layer_off, rows, src, n_q, q_out,
+                  rope, pos, n_pos);
 }
 template <int DH, typename T>
 cudaError_t read_t(Launch L, const Kv4Cache &c, int layer0, int layers, const Kv4Rows &rows, Kv4Tensor k, Kv4Tensor v, long long k_layer, long long v_layer) {
-  const int per = 256 * 8 / DH;
-  return launch_k(kv4_read_kernel<DH, T>, dim3(rows.total, (2 * c.n_kv_heads + per - 1) / per, layers), dim3(256), 0, L.st, L.pdl, c, layer0, rows, k, v,
-                  k_layer, v_layer);
+  const int per = 256 * 8 / DH, slices = (2 * c.n_kv_heads + per - 1) / per;
+  if (many_rows(rows.total, slices * layers))
+    return launch_k(kv4_read_kernel<DH, true, T>, dim3((rows.total + BLOCK_ROWS - 1) / BLOCK_ROWS, slices, layers), dim3(256), 0, L.st, L.pdl, c, layer0, rows,
+                    k, v, k_layer, v_layer);
+  return launch_k(kv4_read_kernel<DH, false, T>, dim3(rows.total, slices, layers), dim3(256), 0, L.st, L.pdl, c, layer0, rows, k, v, k_layer, v_layer);
+}
+template <int DH> cudaError_t move_t(Launch L, const Kv4Cache &c, int B, const Kv4Moves &m) {
+  const int NW = DH / 4 + 2, pairs = c.n_layers * c.n_kv_heads;
+  if (m.n * NW <= 32 * HELD) {
+    // four pairs a warp where that gives every SM two blocks
+    int per = MOVE_WARPS;
+    while (per < 4 * MOVE_WARPS && (long long)B * pairs >= (long long)2 * per * 2 * NUM_SMS) per *= 2;
+    return launch_k(kv4_move_kernel<DH, true>, dim3((pairs + per - 1) / per, B), dim3(32 * MOVE_WARPS), 0, L.st, L.pdl, c, m, per);
+  }
+  return launch_k(kv4_move_kernel<DH, false>, dim3(pairs, B), dim3(32 * MOVE_WARPS), (size_t)m.n * NW * sizeof(uint32_t), L.st, L.pdl, c, m, 1);
 }
 
 }  // namespace
@@ -262,10 +351,6 @@ cudaError_t kv4_read(Launch L, int dh, int dtype, const Kv4Cache &c, int layer0,
                      long long v_layer) {
   return KV4_DISPATCH(dh, dtype, read_t, L, c, layer0, layers, rows, k, v, k_layer, v_layer);
 }
-cudaError_t kv4_move(Launch L, int dh, const Kv4Cache &c, int B, const Kv4Moves &m) {
-  const dim3 grid(c.n_kv_heads, B, c.n_layers);
-  const size_t smem = (size_t)m.n * (2 * (dh / 8) + 2) * sizeof(uint32_t);
-  return dh == 128 ? launch_k(kv4_move_kernel<128>, grid, dim3(128), smem, L.st, L.pdl, c, m) : launch_k(kv4_move_kernel<64>, grid, dim3(128), smem, L.st, L.pdl, c, m);
-}
+cudaError_t kv4_move(Launch L, int dh, const Kv4Cache &c, int B, const Kv4Moves &m) { return dh == 128 ? move_t<128>(L, c, B, m) : move_t<64>(L, c, B, m); }
 
 }  // namespace koala

@@ -77,17 +77,16 @@ struct Kv4Rows {
     if (bad) report();
     count = bad ? 0 : end - first;
   }
-  // sequence of row r (-1: behind the last one); to be called by whole warps
-  __device__ __forceinline__ int sequence_of(int r, int lane) const {
+  // sequence that row r belongs to, or -1
+  __device__ __forceinline__ int sequence_of(int r) const {
     if (row_start == nullptr) return r / max_rows;
-    int n = 0;
-    for (int j = 0; j < B; j += 32) {                      // sequences that end at or before r
-      const bool past = j + lane < B && row_start[j + lane + 1] <= r;
-      const int k = __popc(__ballot_sync(0xffffffffu, past));
-      n += k;
-      if (k < 32) break;
+    int lo = 0, hi = B;                                    // row_start[lo] <= r < row_start[hi], if it is in order
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (row_start[mid] <= r) lo = mid;
+      else hi = mid;
     }
-    return n < B && row_start[n] <= r ? n : -1;
+    return row_start[lo] <= r && r < row_start[lo + 1] ? lo : -1;
   }
   // an impossible row_start need not give any row to anybody: one block looks at all of it
   __device__ __forceinline__ void check() const {
@@ -108,6 +107,31 @@ struct Kv4Tensor {
   void *p;
   long long row, head;
 };
+// Where row r lies: its slot and page; page -1: it is to be left out.
+struct Kv4Place {
+  int slot, page, first, i, count;
+};
+__device__ __forceinline__ Kv4Place kv4_place(const Kv4Cache &c, const Kv4Rows &rows, int r) {
+  Kv4Place p{-1, -1, 0, 0, 0};
+  if (r >= rows.total) return p;
+  const int b = rows.sequence_of(r);
+  if (b < 0) return p;
+  rows.range(b, p.first, p.count);
+  p.i = r - p.first;
+  if (p.i < 0 || p.i >= p.count) return p;
+  p.slot = rows.slot != nullptr ? rows.slot[r] : rows.ctx_len[b] + p.i;
+  if (p.slot < 0) {
+    if (rows.slot == nullptr) rows.report();
+    return p;
+  }
+  p.page = c.page_of(rows.cache_of(b), p.slot >> 4);
+  if ((unsigned)p.page >= (unsigned)c.n_pages) {
+    rows.report();
+    p.page = -1;
+  }
+  return p;
+}
+
 enum { KV4_FP32 = 0, KV4_BF16 = 1, KV4_FP16 = 2, KV4_PAIR = 3 };   // PAIR: output as two bf16 tensors, value and rounding residual
 
 }  // namespace koala
