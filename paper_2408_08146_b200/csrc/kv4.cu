@@ -30,10 +30,19 @@ template <typename T> __device__ __forceinline__ void store4(T *p, const float *
 // Where the new rows come from: the caller's tensors, or the partial sums of the Q/K/V multiply.
 template <typename T> struct FromTensors {
   Kv4Tensor q, k, v;
-  __device__ __forceinline__ void load(int which, int r, int h, int c, float *a) const {
-    const void *p = which == 0 ? q.p : which == 1 ? k.p : v.p;
-    const long long row = which == 0 ? q.row : which == 1 ? k.row : v.row, head = which == 0 ? q.head : which == 1 ? k.head : v.head;
-    load4(reinterpret_cast<const T *>(p) + (long long)r * row + (long long)h * head + c, a);
+  // what a thread needs of the vectors `which` (q, k, v) of head h from element c on
+  struct Column {
+    const T *p;
+    long long row;
+    __device__ __forceinline__ void load(int r, float *a, float *e, int half) const {
+      const T *x = p + r * row;
+      load4(x, a);
+      load4(x + half, e);
+    }
+  };
+  __device__ __forceinline__ Column column(int which, int h, int c) const {
+    const Kv4Tensor &t = which == 0 ? q : which == 1 ? k : v;
+    return Column{reinterpret_cast<const T *>(t.p) + (long long)h * t.head + c, t.row};
   }
 };
 
@@ -48,16 +57,25 @@ __device__ __forceinline__ void rotate4(float *a, float *b, const float *cs) {
   }
 }
 
+// a / b rounded to nearest, for b's reciprocal y rounded to nearest: the quotient a y is off by an ulp at most, its remainder is exact, and adding
+// remainder times y rounds correctly (Markstein, IBM J. Res. Dev. 34, 1990), as long as nothing leaves the range of normal numbers; here
+// 2^-100 <= b < 2^125, and where the remainder does, a / b is below 2^-20 and its code 0.
+__device__ __forceinline__ float quotient(float a, float b, float y) {
+  const float q = __fmul_rn(a, y);
+  return __fmaf_rn(__fmaf_rn(-b, q, a), y, q);
+}
+
 // Codes of this lane's eight numbers as a word, and the vector's parameters (scale in the low half).
+// A code needs no clamp: zero <= x, and x - zero <= 15 scale (1 + 2^-23).  Its rounding to a whole number is the addition of 1.5 * 2^23,
+// after which it stands in the low bits; the upper bits' constant is taken off the word once.
 template <int DH> __device__ __forceinline__ uint32_t quantise(const float *a, const float *b, uint32_t &params) {
   constexpr int LPV = DH / 8;
-  float lo = a[0], hi = a[0];
-  bool bad = false;
+  float lo = a[0], hi = a[0], odd = 0.f;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     lo = fminf(lo, fminf(a[i], b[i]));
     hi = fmaxf(hi, fmaxf(a[i], b[i]));
-    bad = bad || !(fabsf(a[i]) < INFINITY) || !(fabsf(b[i]) < INFINITY);
+    odd = fmaf(b[i], 0.f, fmaf(a[i], 0.f, odd));            // NaN where something is not finite
   }
 #pragma unroll
   for (int o = LPV / 2; o > 0; o >>= 1) {
@@ -65,24 +83,23 @@ template <int DH> __device__ __forceinline__ uint32_t quantise(const float *a, c
     hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
   }
   const unsigned group = (LPV == 16 ? 0xffffu : 0xffu) << ((threadIdx.x & 31) / LPV * LPV);
-  bad = (__ballot_sync(0xffffffffu, bad) & group) != 0u;
   const bf16 z = __float2bfloat16_rd(lo);
   const float zero = __bfloat162float(z);
   bf16 s = __float2bfloat16_ru(__fdiv_rn(__fsub_rn(hi, zero), 15.f));
   const float scale = __bfloat162float(s);
-  bad = bad || !(scale < INFINITY);
+  const bool bad = (__ballot_sync(0xffffffffu, odd != 0.f) & group) != 0u || !(scale < INFINITY);
   const bool flat = scale < 7.888609052210118e-31f;       // 2^-100
   if (flat) s = __float2bfloat16_rn(0.f);
   params = bad ? 0x7fff7fffu : (uint32_t)__bfloat16_as_ushort(s) | (uint32_t)__bfloat16_as_ushort(z) << 16;
   if (flat || bad) return 0u;
+  const float y = __frcp_rn(scale);
   uint32_t w = 0u;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const float ca = fminf(fmaxf(__fdiv_rn(__fsub_rn(a[i], zero), scale), 0.f), 15.f);
-    const float cb = fminf(fmaxf(__fdiv_rn(__fsub_rn(b[i], zero), scale), 0.f), 15.f);
-    w |= (uint32_t)__float2int_rn(ca) << (4 * i) | (uint32_t)__float2int_rn(cb) << (16 + 4 * i);
+    w += __float_as_uint(quotient(__fsub_rn(a[i], zero), scale, y) + 12582912.f) << (4 * i);
+    w += __float_as_uint(quotient(__fsub_rn(b[i], zero), scale, y) + 12582912.f) << (16 + 4 * i);
   }
-  return w;
+  return w - 0x4b400000u * 0x1111u - (0x4b400000u << 16) * 0x1111u;
 }
 
 // Rows of a block: their places are looked up by a lane each, which takes four dependent loads (3 us of the 3.6 us that a block with one
@@ -92,9 +109,9 @@ constexpr int BLOCK_ROWS = 16, ROWS_AT_ONCE = 4;
 // grid (blocks of rows, groups of vectors): a block takes 256 * 8 / DH of the rows' n_q + 2 n_kv vectors.
 // Bound: bytes (append_prompt MEASURE).  MANY: BLOCK_ROWS rows a block, else one.
 template <int DH, bool MANY, typename Src, typename TQ>
-__global__ void __launch_bounds__(256) kv4_append_kernel(Kv4Cache c, size_t layer_off, Kv4Rows rows, Src src, int n_q, Kv4Tensor q_out,
+__global__ void __launch_bounds__(256, MANY ? 4 : 1) kv4_append_kernel(Kv4Cache c, size_t layer_off, Kv4Rows rows, Src src, int n_q, Kv4Tensor q_out,
                                                          const float *rope, const int32_t *pos, int n_pos) {
-  constexpr int LPV = DH / 8, RB = MANY ? BLOCK_ROWS : 1, AT = MANY ? ROWS_AT_ONCE : 1;
+  constexpr int LPV = DH / 8, RB = MANY ? BLOCK_ROWS : 1, AT = MANY ? ROWS_AT_ONCE / 2 : 1;
   pdl_launch_dependents();
   pdl_wait();
   rows.check();
@@ -125,6 +142,9 @@ __global__ void __launch_bounds__(256) kv4_append_kernel(Kv4Cache c, size_t laye
     }
   const bool any_kv = __any_sync(0xffffffffu, which != 0);       // warps of nothing but queries have nothing to quantise
   unsigned char *base = c.pages + layer_off;
+  const auto column = src.column(live ? which : 1, live ? h : 0, 4 * l);
+  TQ *const to_q = which == 0 ? reinterpret_cast<TQ *>(q_out.p) + (long long)h * q_out.head + 4 * l : nullptr;
+  const float *const turns = rope == nullptr || which == 2 ? nullptr : rope + 8 * l;
 #pragma unroll 1
   for (int j0 = 0; j0 < RB; j0 += AT) {
     float a[AT][4], e[AT][4];
@@ -138,12 +158,9 @@ __global__ void __launch_bounds__(256) kv4_append_kernel(Kv4Cache c, size_t laye
       const bool use = live && page[k] >= 0;
 #pragma unroll
       for (int x = 0; x < 4; ++x) a[k][x] = e[k][x] = 0.f;
-      if (use) {
-        src.load(which, r0 + j0 + k, h, 4 * l, a[k]);
-        src.load(which, r0 + j0 + k, h, DH / 2 + 4 * l, e[k]);
-      }
-      if (rope != nullptr && use && which < 2) {
-        const float4 *t = reinterpret_cast<const float4 *>(rope + ((size_t)p * (DH / 2) + 4 * l) * 2);
+      if (use) column.load(r0 + j0 + k, a[k], e[k], DH / 2);
+      if (turns != nullptr && use) {
+        const float4 *t = reinterpret_cast<const float4 *>(turns + (size_t)p * DH);
         cs[k][0] = t[0];
         cs[k][1] = t[1];
       } else {
@@ -154,9 +171,9 @@ __global__ void __launch_bounds__(256) kv4_append_kernel(Kv4Cache c, size_t laye
     for (int k = 0; k < AT; ++k) {
       if (page[k] < 0) continue;           // (the same for the whole block)
       const int r = r0 + j0 + k;
-      if (rope != nullptr && which < 2) rotate4(a[k], e[k], &cs[k][0].x);
+      if (turns != nullptr) rotate4(a[k], e[k], &cs[k][0].x);
       if (live && which == 0) {
-        TQ *o = reinterpret_cast<TQ *>(q_out.p) + (long long)r * q_out.row + (long long)h * q_out.head + 4 * l;
+        TQ *o = to_q + r * q_out.row;
         store4(o, a[k]);
         store4(o + DH / 2, e[k]);
       }
@@ -274,15 +291,25 @@ __global__ void __launch_bounds__(32 * MOVE_WARPS) kv4_move_kernel(Kv4Cache c, K
         t[k] = to[i] + at(in_granule[i] >> 8, w);
       }
     }
-    for (int p = blockIdx.x * pairs_per_block + warp; p < end; p += MOVE_WARPS) {
-      unsigned char *base = c.pages + (size_t)(p / c.n_kv_heads) * c.layer_bytes + (p % c.n_kv_heads) * head_bytes;
-      uint32_t held[HELD];
+    auto base_of = [&](int p) { return c.pages + (size_t)(p / c.n_kv_heads) * c.layer_bytes + (p % c.n_kv_heads) * head_bytes; };
+    for (int p = blockIdx.x * pairs_per_block + warp; p < end; p += 2 * MOVE_WARPS) {       // two pairs at a time
+      const bool two = p + MOVE_WARPS < end;
+      unsigned char *b0 = base_of(p), *b1 = base_of(two ? p + MOVE_WARPS : p);
+      uint32_t h0[HELD], h1[HELD];
 #pragma unroll
-      for (int k = 0; k < HELD; ++k) held[k] = f[k] >= 0 ? *reinterpret_cast<const uint32_t *>(base + f[k]) : 0u;
+      for (int k = 0; k < HELD; ++k) {
+        h0[k] = h1[k] = 0u;
+        if (f[k] < 0) continue;
+        h0[k] = *reinterpret_cast<const uint32_t *>(b0 + f[k]);
+        if (two) h1[k] = *reinterpret_cast<const uint32_t *>(b1 + f[k]);
+      }
       __syncwarp();                        // every lane has read
 #pragma unroll
-      for (int k = 0; k < HELD; ++k)
-        if (t[k] >= 0) *reinterpret_cast<uint32_t *>(base + t[k]) = held[k];
+      for (int k = 0; k < HELD; ++k) {
+        if (t[k] < 0) continue;
+        *reinterpret_cast<uint32_t *>(b0 + t[k]) = h0[k];
+        if (two) *reinterpret_cast<uint32_t *>(b1 + t[k]) = h1[k];
+      }
       __syncwarp();
     }
   } else {
@@ -329,9 +356,9 @@ cudaError_t read_t(Launch L, const Kv4Cache &c, int layer0, int layers, const Kv
 template <int DH> cudaError_t move_t(Launch L, const Kv4Cache &c, int B, const Kv4Moves &m) {
   const int NW = DH / 4 + 2, pairs = c.n_layers * c.n_kv_heads;
   if (m.n * NW <= 32 * HELD) {
-    // four pairs a warp where that gives every SM two blocks
+    // two pairs a warp where that leaves every SM four blocks
     int per = MOVE_WARPS;
-    while (per < 4 * MOVE_WARPS && (long long)B * pairs >= (long long)2 * per * 2 * NUM_SMS) per *= 2;
+    while (per < 4 * MOVE_WARPS && (long long)B * pairs >= (long long)2 * per * 4 * NUM_SMS) per *= 2;
     return launch_k(kv4_move_kernel<DH, true>, dim3((pairs + per - 1) / per, B), dim3(32 * MOVE_WARPS), 0, L.st, L.pdl, c, m, per);
   }
   return launch_k(kv4_move_kernel<DH, false>, dim3(pairs, B), dim3(32 * MOVE_WARPS), (size_t)m.n * NW * sizeof(uint32_t), L.st, L.pdl, c, m, 1);
