@@ -26,6 +26,8 @@ class koala_kv4_rows(C.Structure):
 
 
 _lib = None
+# the current stream's handle, without the Python object that torch.cuda.current_stream makes (2 us of a call's 9)
+_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
 def _library() -> C.CDLL:
@@ -59,20 +61,29 @@ def rope_table(n_pos: int, head_dim: int, base: float = 10000.0, device="cuda:0"
 class KV4Rows:
     """The rows of one forward (koala_kv4_rows): made once, used by every layer.  Keeps its tensors alive."""
 
-    def __init__(self, c: koala_kv4_rows, total: int, device: torch.device, keep: tuple):
-        self._c, self.total, self.device, self._keep = c, total, device, keep
+    def __init__(self, c: koala_kv4_rows, total: int, geometry: tuple, keep: tuple):
+        self._c, self.total, self._geometry, self._keep = c, total, geometry, keep
+        self._scratch = {}                  # bytes by number of heads
         self._p = C.addressof(c)
 
 
-def _strides(t: torch.Tensor, rows: int, heads: int, dim: int, dtype: torch.dtype, device: torch.device, name: str) -> Tuple[int, int, int]:
+def _wrong(t: torch.Tensor, shape, dtype, device, name: str):
     if t.dtype is not dtype or t.device != device:
         raise ValueError(f"{name} must be a {dtype} tensor on {device}")
-    if t.dim() != 3 or t.size(0) != rows or t.size(1) != heads or t.size(2) != dim:
-        raise ValueError(f"{name} must have the shape {(rows, heads, dim)}, not {tuple(t.shape)}")
+    if tuple(t.shape) != shape:
+        raise ValueError(f"{name} must have the shape {shape}, not {tuple(t.shape)}")
+    raise ValueError(f"{name}: the last dimension must be contiguous, addresses and strides multiples of 4 elements")
+
+
+def _strides(t: torch.Tensor, shape, dtype: torch.dtype, index: int, device: torch.device, name: str) -> Tuple[int, int, int]:
+    """Address and strides of a [rows][heads][head_dim] tensor; index: the device's, -1 for the CPU.  (Every call of every layer comes here.)"""
+    if t.dtype is not dtype or t.get_device() != index or t.shape != shape:
+        _wrong(t, shape, dtype, device, name)
+    at = t.data_ptr()
     a, b, c = t.stride()
-    if c != 1 or a % 4 or b % 4 or t.data_ptr() % (4 * t.element_size()):
-        raise ValueError(f"{name}: the last dimension must be contiguous, addresses and strides multiples of 4 elements")
-    return t.data_ptr(), a, b
+    if c != 1 or (a | b) & 3 or at & (15 if dtype is torch.float32 else 7):
+        _wrong(t, shape, dtype, device, name)
+    return at, a, b
 
 
 class PagedKV4:
@@ -99,6 +110,8 @@ class PagedKV4:
         self.pages = pages
         c.pages = pages.data_ptr()
         self._c, self._p = c, C.addressof(c)
+        self._index = dev.index if dev.type == "cuda" else -1
+        self._geometry = (self._index, n_kv_heads, head_dim, page_size)      # what a plan of rows depends on
 
     # ------------------------------------------------------------------ plans
     def _ints(self, t: Optional[torch.Tensor], shape: Tuple[int, ...], name: str, dtype=torch.int32):
@@ -134,22 +147,22 @@ class PagedKV4:
         c = koala_kv4_rows(C.sizeof(koala_kv4_rows), B, total, max_rows, stride, at, self._ints(ctx_len, (B,), "ctx_len"),
                            self._ints(row_start, (B + 1,), "row_start"), self._ints(kv_len, (B,), "kv_len"), self._ints(slot, (total,), "slot"),
                            self._ints(mask, (total, 2), "mask", torch.int64), self._ints(status, (1,), "status"))
-        return KV4Rows(c, total, self.device, (page_table, ctx_len, row_start, kv_len, slot, mask, status))
+        return KV4Rows(c, total, self._geometry, (page_table, ctx_len, row_start, kv_len, slot, mask, status))
 
     # ------------------------------------------------------------------ the four calls
     def _call(self, name: str, fn, *args):
-        dev = self.device
-        if torch.cuda.current_device() != dev.index:
-            with torch.cuda.device(dev):
-                rc = fn(self._p, *args, torch.cuda.current_stream(dev).cuda_stream)
+        index = self._index
+        if torch.cuda.current_device() != index:
+            with torch.cuda.device(self.device):
+                rc = fn(self._p, *args, _stream(index))
         else:
-            rc = fn(self._p, *args, torch.cuda.current_stream(dev).cuda_stream)
+            rc = fn(self._p, *args, _stream(index))
         if rc != KOALA_OK:
             raise KoalaError(rc, name)
 
     def _mine(self, rows: KV4Rows):
-        if rows.device != self.device:
-            raise ValueError(f"the rows are on {rows.device}, the cache on {self.device}")
+        if rows._geometry != self._geometry:
+            raise ValueError(f"rows for a cache with (device, kv heads, head dim, page size) {rows._geometry}, not {self._geometry}")
 
     def append(self, layer: int, rows: KV4Rows, k: torch.Tensor, v: torch.Tensor, rope: Optional[torch.Tensor] = None,
                pos: Optional[torch.Tensor] = None, q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
@@ -157,16 +170,18 @@ class PagedKV4:
         k, v: [total][n_kv_heads][head_dim]; q, q_out: [total][heads][head_dim], all of one type (fp32, bf16, fp16).  rope:
         [positions][head_dim / 2][2] fp32 (rope_table); pos: int32 [total] positions, by default the slots."""
         self._mine(rows)
-        n, dt, dim, dev = rows.total, k.dtype, self.head_dim, self.device
+        n, dt, dim, dev, index = rows.total, k.dtype, self.head_dim, self.device, self._index
         if dt not in _TYPES:
             raise ValueError(f"keys of type {dt}")
-        a = _strides(k, n, self.n_kv_heads, dim, dt, dev, "k") + _strides(v, n, self.n_kv_heads, dim, dt, dev, "v")
+        shape = (n, self.n_kv_heads, dim)
+        a = _strides(k, shape, dt, index, dev, "k") + _strides(v, shape, dt, index, dev, "v")
         heads = 0
         if q is not None:
             heads = q.size(1)
             if q_out is None:
                 q_out = torch.empty(q.shape, dtype=dt, device=dev)
-            a += _strides(q, n, heads, dim, dt, dev, "q") + _strides(q_out, n, heads, dim, dt, dev, "q_out")
+            shape = (n, heads, dim)
+            a += _strides(q, shape, dt, index, dev, "q") + _strides(q_out, shape, dt, index, dev, "q_out")
         else:
             a += (0, 0, 0, 0, 0, 0)
         table, n_pos = None, 0
@@ -188,9 +203,12 @@ class PagedKV4:
             raise ValueError(f"queries of type {dt}")
         if out is None:
             out = torch.empty(q.shape, dtype=dt, device=dev)
-        t = struct.pack("6q", *_strides(q, rows.total, heads, dim, dt, dev, "q"), *_strides(out, rows.total, heads, dim, dt, dev, "out"))
+        shape = (rows.total, heads, dim)
+        t = struct.pack("6q", *_strides(q, shape, dt, self._index, dev, "q"), *_strides(out, shape, dt, self._index, dev, "out"))
         lib = _library()
-        need = lib.koala_kv4_attention_scratch_bytes(self._p, rows._p, heads)
+        need = rows._scratch.get(heads)
+        if need is None:
+            need = rows._scratch[heads] = self.scratch_bytes(rows, heads)
         at = None
         if need:
             if scratch is None:
@@ -223,10 +241,10 @@ class PagedKV4:
                 if t.dim() != 4 or t.size(0) != self.n_layers or t.stride(0) % 4:
                     raise ValueError(f"{name} must have the shape {shape}, its layers a multiple of 4 elements apart")
                 layers += (t.stride(0),)
-                a += _strides(t[0], n, self.n_kv_heads, dim, dt, dev, name)
+                a += _strides(t[0], shape[1:], dt, self._index, dev, name)
             else:
                 layers += (0,)
-                a += _strides(t, n, self.n_kv_heads, dim, dt, dev, name)
+                a += _strides(t, shape, dt, self._index, dev, name)
             outs.append(t)
         self._call("koala_kv4_read", _library().koala_kv4_read, -1 if layer is None else layer, rows._p, _TYPES[dt], struct.pack("6q", *a),
                    struct.pack("2q", *layers))
