@@ -62,6 +62,9 @@ extern "C" {
                                       at most 128 rows per forward) instead of one kernel per step;
                                       same results up to summation order, measured slower on B200    */
 
+#define KOALA_F_KV4 8u                 /* bf16 configurations: the target's keys and values are held in a paged cache of 4 bits
+                                      (koala_set_kv4); target_k and target_v may be NULL               */
+
 #define KOALA_MAX_TREE 128 /* largest N: ancestor sets are 128-bit masks */
 #define KOALA_MAX_TOPK 16
 #define KOALA_LAYER_TENSORS 9 /* attn_norm, wq, wk, wv, wo, ffn_norm, w_gate, w_up, w_down */
@@ -103,7 +106,7 @@ typedef struct {
 } koala_weights;
 
 typedef struct {
-  void *target_k, *target_v; /* [L][B][n_heads][S_max][head_dim], dtype storage */
+  void *target_k, *target_v; /* [L][B][n_heads][S_max][head_dim], dtype storage; unused with KOALA_F_KV4 */
   void *draft_k, *draft_v;   /* EAGLE: [K][B][n_heads][S_max][head_dim]; else NULL */
   int32_t *seq_len;          /* [B] device: tokens held by the target cache; caller initialises */
   void *workspace;           /* device, 256-byte aligned */
@@ -334,6 +337,13 @@ typedef struct {
   int32_t n_pages;
   void *pages;       /* device, 128-byte aligned, koala_kv4_bytes() bytes: [n_layers][n_pages][page] */
 } koala_kv4;
+
+/* The cache of a context made with KOALA_F_KV4: n_layers = L, n_kv_heads = n_heads, head_dim as the configuration; page_table
+ * (DEVICE [B][table_stride]) names pages for at least S_max slots a sequence, entries that are not reached yet may be anything.  *cache is
+ * copied; pages and table are borrowed.  To be called before the first forward, and again whenever the table or the pages
+ * have moved, between koala_accept and the next call.  The contents of the table may change between calls: they are read when kernels run.
+ * A slot without a page sets the device status to KOALA_E_INVALID. */
+int koala_set_kv4(koala_ctx *ctx, const koala_kv4 *cache, const int32_t *page_table, int32_t table_stride);
 
 /* The rows of one forward: `total` tokens of B sequences, the rows of a sequence next to one another.  All pointers are
  * DEVICE arrays; made once, it serves every layer of the forward. */

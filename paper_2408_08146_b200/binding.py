@@ -20,7 +20,7 @@ ERR_NAMES = {0: "KOALA_OK", 1: "KOALA_E_INVALID", 2: "KOALA_E_UNSUPPORTED", 3: "
              4: "KOALA_E_STATE", 5: "KOALA_E_CUDA", 6: "KOALA_E_TIMEOUT"}
 KOALA_FP32, KOALA_BF16 = 0, 1
 KOALA_EAGLE, KOALA_MEDUSA = 0, 1
-KOALA_F_NO_TENSOR_CORES, KOALA_F_NO_PDL, KOALA_F_LAYER_KERNEL = 1, 2, 4
+KOALA_F_NO_TENSOR_CORES, KOALA_F_NO_PDL, KOALA_F_LAYER_KERNEL, KOALA_F_KV4 = 1, 2, 4, 8
 LAYER_TENSORS = ("attn_norm", "wq", "wk", "wv", "wo", "ffn_norm", "w_gate", "w_up", "w_down")
 
 
@@ -89,6 +89,8 @@ def load_library(rebuild: bool = False) -> C.CDLL:
     lib.koala_draft.argtypes = [C.c_void_p, C.c_int]
     lib.koala_expand_tree.restype = C.c_int
     lib.koala_expand_tree.argtypes = [C.c_void_p, C.c_int]
+    lib.koala_set_kv4.restype = C.c_int
+    lib.koala_set_kv4.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32]
     lib.koala_verify.restype = C.c_int
     lib.koala_verify.argtypes = [C.c_void_p, C.POINTER(koala_tree)]
     lib.koala_set_sampling.restype = C.c_int
@@ -195,8 +197,11 @@ class Koala:
     """Owns the device buffers of one context and forwards the five calls."""
 
     def __init__(self, cfg, weights: Dict[str, torch.Tensor], static_tree=None, flags: int = 0,
-                 device: str = "cuda:0"):
+                 device: str = "cuda:0", kv4=None):
+        """kv4: (PagedKV4, page_table int32 [B][pages]) - the target's keys and values are held in that paged 4-bit cache."""
         self.lib = load_library()
+        if kv4 is not None:
+            flags |= KOALA_F_KV4
         self.cfg = cfg
         self.dev = torch.device(device)
         self.weights = weights
@@ -205,7 +210,7 @@ class Koala:
         for name, t in weights.items():
             if t.device != self.dev or t.dtype != dt or not t.is_contiguous():
                 raise ValueError(f"weight {name} must be a contiguous {dt} tensor on {self.dev}")
-        kv_shape = (cfg.L, cfg.B, cfg.n_heads, cfg.S_max, cfg.head_dim)
+        kv_shape = (cfg.L, cfg.B, cfg.n_heads, cfg.S_max if kv4 is None else 0, cfg.head_dim)
         self.target_k = torch.zeros(kv_shape, dtype=dt, device=self.dev)
         self.target_v = torch.zeros(kv_shape, dtype=dt, device=self.dev)
         eagle = cfg.head_kind == KOALA_EAGLE
@@ -241,7 +246,7 @@ class Koala:
                 raise ValueError("Medusa-style heads need a static tree (parent, level, rank)")
             self._st = [_i32_array(a) for a in static_tree]
             w.static_parent, w.static_level, w.static_rank = (C.cast(a, C.POINTER(C.c_int32)) for a in self._st)
-        st = koala_state(self.target_k.data_ptr(), self.target_v.data_ptr(),
+        st = koala_state(self.target_k.data_ptr() if kv4 is None else None, self.target_v.data_ptr() if kv4 is None else None,
                          self.draft_k.data_ptr() if eagle and cfg.K > 0 else None,
                          self.draft_v.data_ptr() if eagle and cfg.K > 0 else None,
                          self.seq_len.data_ptr(), self.workspace.data_ptr() + self._ws_off, nbytes)
@@ -253,6 +258,8 @@ class Koala:
             self.lib.koala_destroy(self._ctx)
             self._ctx = C.c_void_p(None)
             raise KoalaError(rc, text)
+        if kv4 is not None:
+            self.set_kv4(*kv4)
         self.out_stride = max(cfg.N, cfg.D + 1)
         self.out_tokens = torch.zeros(cfg.B, self.out_stride, dtype=torch.int32, device=self.dev)
         self.out_len = torch.zeros(cfg.B, dtype=torch.int32, device=self.dev)
@@ -262,6 +269,15 @@ class Koala:
     def _check(self, rc: int):
         if rc != KOALA_OK:
             raise KoalaError(rc, self.lib.koala_last_error(self._ctx).decode())
+
+    def set_kv4(self, cache, page_table: torch.Tensor):
+        """The paged 4-bit cache of the target and its page table (again whenever either has moved)."""
+        if page_table.dtype is not torch.int32 or page_table.device != self.dev or page_table.dim() != 2 or page_table.size(0) != self.cfg.B or not page_table.is_contiguous():
+            raise ValueError(f"page_table must be a contiguous int32 tensor [{self.cfg.B}][pages] on {self.dev}")
+        if cache.device != self.dev:
+            raise ValueError(f"the cache is on {cache.device}")
+        self._check(self.lib.koala_set_kv4(self._ctx, cache._p, page_table.data_ptr(), page_table.size(1)))
+        self.kv4 = (cache, page_table)
 
     def koala_draft(self, p: int):
         self._check(self.lib.koala_draft(self._ctx, p))

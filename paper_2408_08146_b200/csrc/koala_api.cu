@@ -10,10 +10,12 @@
 #include "../../include/koala.h"
 #include "common.cuh"
 #include "koala_debug.h"
+#include "kv4.h"
 
 using namespace koala;
 
 namespace koala {
+bool kv4_describe(const koala_kv4 *k, const int32_t *table, int table_stride, Kv4Cache *out);      // kv4_api.cu
 void tc_forget_maps();
 void tc_set_tuning(int key, int value);
 unsigned long long g_launches = 0;
@@ -77,6 +79,10 @@ struct koala_ctx {
   unsigned *layer_sync;   // device counters of the persistent layer kernel
   unsigned layer_use[LAYER_MAX_PHASES];   // how often each counter has been used (host)
   bool stream_layers;     // decoder layers run through the persistent layer kernel where it applies
+  bool kv4;               // the target's keys and values are in a paged 4-bit cache ..
+  bool kv4_set;           // .. which has been given
+  Kv4Cache kv4_cache;
+  float *kv4_scratch;
   RowScale pending;       // scale still owed by the consumer of the GEMM that reads c->xn
   float *x, *qbuf, *P, *verify_logits, *draft_logits, *verify_hid, *feat[2], *mx;
   Operand xn, attn_out, act, cat, lmin;
@@ -157,6 +163,7 @@ bool config_ok(const koala_config *cfg, char *why, size_t n) {
     if ((cfg->D - 1) * cfg->topk > 128) BAD("EAGLE: (D-1)*topk must be <= 128");
   }
   if (!(cfg->rms_eps > 0.f) || !(cfg->rope_base > 1.f)) BAD("bad rms_eps / rope_base");
+  if ((cfg->flags & KOALA_F_KV4) != 0 && cfg->dtype != KOALA_BF16) BAD("KOALA_F_KV4 needs bf16");
 #undef BAD
   return true;
 }
@@ -207,6 +214,7 @@ size_t carve(koala_ctx *c, const koala_config &cfg, unsigned char *base) {
     c->qpair.hi = w.take<unsigned char>((size_t)Mp * H * esz);
     c->qpair.lo = w.take<unsigned char>((size_t)Mp * H * esz);
   }
+  c->kv4_scratch = (cfg.flags & KOALA_F_KV4) != 0 ? w.take<float>(kv4_attention_scratch(cfg.head_dim, NUM_SMS, KOALA_MAX_TREE) / sizeof(float)) : nullptr;
   c->act = operand(F);
   c->cat = operand(2 * H);
   c->lmin = operand(H);
@@ -347,6 +355,26 @@ int run_attention(koala_ctx *c, void *kc, void *vc, int R, int rows_per_seq, boo
   return KOALA_OK;
 }
 
+// The rows of a forward as the calls of the paged 4-bit cache take them.
+Kv4Rows kv4_rows(koala_ctx *c, int R, int rows_per_seq) {
+  const RowPlan p = row_plan(c);
+  return Kv4Rows{R / rows_per_seq, R, rows_per_seq, nullptr, p.ctx_len, p.kv_len, p.slot, p.mask, p.seq, c->status};
+}
+// The rotary step and the attention of target layer `layer` over the paged 4-bit cache.
+int run_kv4(koala_ctx *c, const SplitIn &qkv, int layer, int R, int rows_per_seq, bool kv_only) {
+  const koala_config &g = c->cfg;
+  const Kv4Rows rows = kv4_rows(c, R, rows_per_seq);
+  const size_t off = (size_t)layer * c->kv4_cache.layer_bytes;
+  CU_TRY(kv4_append_sums(LN(c), g.head_dim, c->kv4_cache, off, rows, qkv, c->pending, kv_only ? 0 : g.n_heads, c->qbuf, c->p.rope));
+  if (kv_only) return KOALA_OK;
+  const int ta = time_begin(c, KOALA_CLS_ATTENTION, 0);
+  const Kv4Attn a{c->kv4_cache, off, rows, Kv4Tensor{c->qbuf, g.H, g.head_dim}, Kv4Tensor{c->attn_out.hi, g.H, g.head_dim}, c->attn_out.lo, KV4_FP32, KV4_PAIR,
+                  g.n_heads, 1.f / sqrtf((float)g.head_dim), 0ull, c->kv4_scratch};
+  CU_TRY(kv4_attention(LN(c), g.head_dim, a, NUM_SMS));
+  time_end(c, ta);
+  return KOALA_OK;
+}
+
 // One pre-norm decoder layer over R rows.  On entry x holds the residual stream and xn the input
 // of the attention block: normalised, or x * gain with the scale still pending in c->pending.
 // On exit x is updated; if `defer` the next layer's input is left in c->xn as x * next_g with its
@@ -354,7 +382,7 @@ int run_attention(koala_ctx *c, void *kc, void *vc, int R, int rows_per_seq, boo
 // `out_f32` optionally the same in fp32.  kv_only: the layer's keys and values are all that is wanted.
 int run_layer(koala_ctx *c, const LayerW &w, void *kc, void *vc, int R, int rows_per_seq,
               const void *next_g, Operand next_xn, float *out_f32, RowMap out_map, bool defer,
-              bool kv_only = false) {
+              bool kv_only = false, int kv4_layer = -1) {
   const koala_config &g = c->cfg;
   const int H = g.H, F = g.F;
   const bool can_defer = (H % 4) == 0 && H <= 8192;
@@ -365,10 +393,14 @@ int run_layer(koala_ctx *c, const LayerW &w, void *kc, void *vc, int R, int rows
   // with a row or two per sequence the attention may take the multiply's partial sums itself (where these turn out to be shared by
   // the deal, as for the 156 tiles of a 33B shape, the rotary launch takes them after all; that the multiply had held its dependents
   // back costs nothing there: six layers, one-token step 1204 us with, 1205 without)
-  const bool few = c->use_tc && g.dtype == KOALA_BF16 && g.head_dim == 128 && c->ingest_blocks == 0 && !kv_only && tc_supported(qkv, H) &&
+  const bool few = c->use_tc && g.dtype == KOALA_BF16 && g.head_dim == 128 && c->ingest_blocks == 0 && !kv_only && kv4_layer < 0 && tc_supported(qkv, H) &&
                    attn_few_takes_sums(rows_per_seq, g.B, g.n_heads, g.S_max, NUM_SMS);
   K_TRY(do_gemm(c, c->xn, H, qkv, R, nullptr, 0, &s, few));
-  if (few && attn_few_rope_supported(s)) {
+  if (kv4_layer >= 0) {
+    K_TRY(run_kv4(c, s, kv4_layer, R, rows_per_seq, kv_only));
+    c->pending = none;
+    if (kv_only) return KOALA_OK;
+  } else if (few && attn_few_rope_supported(s)) {
     const int ta = time_begin(c, KOALA_CLS_ATTENTION, 0);
     CU_TRY(tree_attention_few_rope(LN(c), s, c->pending, kc, vc, row_plan(c), c->attn_out, rows_per_seq, g.B, g.n_heads, g.S_max, NUM_SMS));
     time_end(c, ta);
@@ -488,7 +520,8 @@ int run_layers(koala_ctx *c, const std::vector<LayerW> &layers, int n_layers, vo
   const size_t le = kv_layer_elems(g) * c->esz;
   auto kc_of = [&](int l) { return (void *)((unsigned char *)kbase + (size_t)l * le); };
   auto vc_of = [&](int l) { return (void *)((unsigned char *)vbase + (size_t)l * le); };
-  bool streamed = c->stream_layers && g.dtype == KOALA_BF16 && c->pair && g.head_dim == 128 && R <= 128 &&
+  const bool kv4 = c->kv4 && &layers == &c->layers;      // the target's layers
+  bool streamed = !kv4 && c->stream_layers && g.dtype == KOALA_BF16 && c->pair && g.head_dim == 128 && R <= 128 &&
                   c->qpair.lo != nullptr && n_layers > 0 && c->ingest_blocks == 0;
   LayerJob job;
     auto base_job = [&]() {
@@ -545,7 +578,7 @@ int run_layers(koala_ctx *c, const std::vector<LayerW> &layers, int n_layers, vo
     for (int l = 0; l < n_layers; ++l) {
       const bool last = l == n_layers - 1;
       K_TRY(run_layer(c, layers[l], kc_of(l), vc_of(l), R, rows_per_seq, last ? final_g : layers[l + 1].attn_norm,
-                      last ? final_xn : c->xn, last ? out_f32 : nullptr, out_map, !last, last && last_kv_only));
+                      last ? final_xn : c->xn, last ? out_f32 : nullptr, out_map, !last, last && last_kv_only, kv4 ? l : -1));
     }
     return KOALA_OK;
   }
@@ -786,6 +819,17 @@ int draft_eagle(koala_ctx *c, int pass) {
   return KOALA_OK;
 }
 
+// The accepted nodes' keys and values to their places, their hidden states to the pending rows.
+int compact(koala_ctx *c) {
+  const koala_config &g = c->cfg;
+  if (c->kv4) {
+    const Kv4Moves m{c->pend_cap, g.N, c->t.acc_path, nullptr, c->t.acc_S, c->t.acc_len, c->status};      // no path is longer than pend_cap
+    CU_TRY(kv4_move(LN(c), g.head_dim, c->kv4_cache, g.B, m));
+  }
+  CU_TRY(kv_compact(LN(c), g.dtype, c->t, c->verify_hid, c->tk, c->tv, c->kv4 ? 0 : g.L, g.B, g.N, g.n_heads, g.head_dim, g.S_max));
+  return KOALA_OK;
+}
+
 int draft_medusa(koala_ctx *c) {
   const koala_config &g = c->cfg;
   const int H = g.H, B = g.B, nh = g.n_medusa_heads;
@@ -884,7 +928,9 @@ int koala_init(const koala_config *cfg, const koala_weights *w, const koala_stat
   const koala_config &g = c->cfg;
   if (!w->embed || !w->lm_head || !w->final_norm || !w->layer_w)
     return fail(c, KOALA_E_INVALID, "missing target weights");
-  if (!st->target_k || !st->target_v || !st->seq_len || !st->workspace)
+  c->kv4 = (g.flags & KOALA_F_KV4) != 0;
+  c->kv4_set = false;
+  if ((!c->kv4 && (!st->target_k || !st->target_v)) || !st->seq_len || !st->workspace)
     return fail(c, KOALA_E_INVALID, "missing state pointers");
   if (((uintptr_t)st->workspace & 255u) != 0) return fail(c, KOALA_E_INVALID, "workspace not 256-byte aligned");
   c->st = (cudaStream_t)cuda_stream;
@@ -1024,8 +1070,24 @@ int koala_expand_tree(koala_ctx *c, int pass) {
   return KOALA_OK;
 }
 
+int koala_set_kv4(koala_ctx *c, const koala_kv4 *cache, const int32_t *page_table, int32_t table_stride) {
+  if (!c) return KOALA_E_INVALID;
+  const koala_config &g = c->cfg;
+  if (!c->kv4) return fail(c, KOALA_E_STATE, "the context was not made with KOALA_F_KV4");
+  Kv4Cache view;
+  if (!kv4_describe(cache, page_table, table_stride, &view)) return fail(c, KOALA_E_INVALID, "bad description of the 4-bit cache");
+  if (cache->n_layers != g.L || cache->n_kv_heads != g.n_heads || cache->head_dim != g.head_dim)
+    return fail(c, KOALA_E_INVALID, "4-bit cache of %d layers, %d heads of %d; the target has %d, %d, %d", cache->n_layers, cache->n_kv_heads,
+                cache->head_dim, g.L, g.n_heads, g.head_dim);
+  if ((long long)table_stride * cache->page_size < g.S_max) return fail(c, KOALA_E_CAPACITY, "a page-table row names fewer than S_max = %d slots", g.S_max);
+  c->kv4_cache = view;
+  c->kv4_set = true;
+  return KOALA_OK;
+}
+
 int koala_verify(koala_ctx *c, const koala_tree *tree) {
   if (!c) return KOALA_E_INVALID;
+  if (c->kv4 && !c->kv4_set) return fail(c, KOALA_E_STATE, "koala_set_kv4 must come first");
   const koala_config &g = c->cfg;
   if (tree) {
     if (!tree->tok || !tree->parent || !tree->n_nodes) return fail(c, KOALA_E_INVALID, "null tree arrays");
@@ -1060,6 +1122,7 @@ int koala_verify(koala_ctx *c, const koala_tree *tree) {
 int koala_ingest(koala_ctx *c, const int32_t *tok, int32_t stride, const int32_t *len, int32_t n_parts) {
   if (!c) return KOALA_E_INVALID;
   const koala_config &g = c->cfg;
+  if (c->kv4 && !c->kv4_set) return fail(c, KOALA_E_STATE, "koala_set_kv4 must come first");
   if (!tok || !len || n_parts < 1) return fail(c, KOALA_E_INVALID, "null prompt / no parts");
   IngestLens k;
   memset(&k, 0, sizeof(k));
@@ -1104,7 +1167,7 @@ int koala_accept(koala_ctx *c, const int32_t *forced_len, int32_t *out_tokens, i
   if (!out_tokens || !out_len || out_stride < 1) return fail(c, KOALA_E_INVALID, "null outputs");
   if (c->phase != PH_VERIFIED) return fail(c, KOALA_E_STATE, "koala_accept must follow koala_verify");
   CU_TRY(accept_walk(LN(c), c->t, c->verify_tgt, forced_len, c->seq_len, out_tokens, out_stride, out_len, g.B, g.N));
-  CU_TRY(kv_compact(LN(c), g.dtype, c->t, c->verify_hid, c->tk, c->tv, g.L, g.B, g.N, g.n_heads, g.head_dim, g.S_max));
+  K_TRY(compact(c));
   c->phase = PH_READY;
   c->last_pass = -1;
   return KOALA_OK;
@@ -1129,7 +1192,7 @@ int koala_accept_sampled(koala_ctx *c, const float *u_accept, const float *u_bon
     return fail(c, KOALA_E_STATE, "koala_accept_sampled must follow koala_verify of the drafted chain");
   CU_TRY(accept_sampled(LN(c), c->t, c->verify_logits, c->chain_d, u_accept, u_bonus, c->seq_len, out_tokens, out_stride,
                         out_len, g.B, g.N, g.V, g.D, c->status));
-  CU_TRY(kv_compact(LN(c), g.dtype, c->t, c->verify_hid, c->tk, c->tv, g.L, g.B, g.N, g.n_heads, g.head_dim, g.S_max));
+  K_TRY(compact(c));
   c->phase = PH_READY;
   c->last_pass = -1;
   return KOALA_OK;

@@ -46,6 +46,34 @@ template <typename T> struct FromTensors {
   }
 };
 
+// The partial sums of the Q/K/V multiply: columns q | k | v of `width` each, every row with a scale owed by the norm before.
+struct FromSums {
+  SplitIn s;
+  RowScale sc;
+  int width, dh;
+  struct Column {
+    const FromSums *f;
+    int c;
+    __device__ __forceinline__ void load(int r, float *a, float *e, int half) const {
+      const SplitIn &s = f->s;
+      const float scale = f->sc.of(r);
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const int at = c + x * half, n = s.count(r, at);
+        const float *q = s.p + (size_t)r * s.ld + at;
+        float4 v = *reinterpret_cast<const float4 *>(q);
+        for (int k = 1; k < n; ++k) {                     // in slot order
+          const float4 u = *reinterpret_cast<const float4 *>(q + (size_t)k * s.stride);
+          v.x += u.x; v.y += u.y; v.z += u.z; v.w += u.w;
+        }
+        float *o = x == 0 ? a : e;
+        o[0] = v.x * scale; o[1] = v.y * scale; o[2] = v.z * scale; o[3] = v.w * scale;
+      }
+    }
+  };
+  __device__ __forceinline__ Column column(int which, int h, int c) const { return Column{this, which * width + h * dh + c}; }
+};
+
 // One vector of a row: DH / 8 lanes, lane l with dims 4l .. 4l+3 (a) and DH/2 + 4l .. (b).
 // The products of the rotation are rounded one by one, so that codes do not depend on how a compiler contracts them.
 __device__ __forceinline__ void rotate4(float *a, float *b, const float *cs) {
@@ -110,7 +138,7 @@ constexpr int BLOCK_ROWS = 16, ROWS_AT_ONCE = 4;
 // Bound: bytes (append_prompt MEASURE).  MANY: BLOCK_ROWS rows a block, else one.
 template <int DH, bool MANY, typename Src, typename TQ>
 __global__ void __launch_bounds__(256, MANY ? 4 : 1) kv4_append_kernel(Kv4Cache c, size_t layer_off, Kv4Rows rows, Src src, int n_q, Kv4Tensor q_out,
-                                                         const float *rope, const int32_t *pos, int n_pos) {
+                                                         const float *rope, const int32_t *pos, int n_pos, int by_row) {
   constexpr int LPV = DH / 8, RB = MANY ? BLOCK_ROWS : 1, AT = MANY ? ROWS_AT_ONCE / 2 : 1;
   pdl_launch_dependents();
   pdl_wait();
@@ -125,7 +153,7 @@ __global__ void __launch_bounds__(256, MANY ? 4 : 1) kv4_append_kernel(Kv4Cache 
   int turn = 0;
   if (lane < RB) {
     mine = kv4_place(c, rows, r0 + lane);
-    turn = pos != nullptr && mine.page >= 0 ? pos[r0 + lane] : mine.slot;
+    turn = by_row ? r0 + lane : pos != nullptr && mine.page >= 0 ? pos[r0 + lane] : mine.slot;
     if (mine.page >= 0 && rope != nullptr && (unsigned)turn >= (unsigned)n_pos) {
       rows.report();
       mine.page = -1;
@@ -341,9 +369,18 @@ cudaError_t append_t(Launch L, const Kv4Cache &c, size_t layer_off, const Kv4Row
   const int slices = (n_vec + per - 1) / per;
   if (many_rows(rows.total, slices))
     return launch_k(kv4_append_kernel<DH, true, FromTensors<T>, T>, dim3((rows.total + BLOCK_ROWS - 1) / BLOCK_ROWS, slices), dim3(256), 0, L.st, L.pdl, c,
-                    layer_off, rows, src, n_q, q_out, rope, pos, n_pos);
+                    layer_off, rows, src, n_q, q_out, rope, pos, n_pos, 0);
   return launch_k(kv4_append_kernel<DH, false, FromTensors<T>, T>, dim3(rows.total, slices), dim3(256), 0, L.st, L.pdl, c, layer_off, rows, src, n_q, q_out,
-                  rope, pos, n_pos);
+                  rope, pos, n_pos, 0);
+}
+template <int DH>
+cudaError_t append_sums_t(Launch L, const Kv4Cache &c, size_t layer_off, const Kv4Rows &rows, const FromSums &src, int n_q, Kv4Tensor q_out, const float *rope) {
+  const int per = 256 * 8 / DH, slices = (n_q + 2 * c.n_kv_heads + per - 1) / per;
+  if (many_rows(rows.total, slices))
+    return launch_k(kv4_append_kernel<DH, true, FromSums, float>, dim3((rows.total + BLOCK_ROWS - 1) / BLOCK_ROWS, slices), dim3(256), 0, L.st, L.pdl, c,
+                    layer_off, rows, src, n_q, q_out, rope, (const int32_t *)nullptr, rows.total, 1);
+  return launch_k(kv4_append_kernel<DH, false, FromSums, float>, dim3(rows.total, slices), dim3(256), 0, L.st, L.pdl, c, layer_off, rows, src, n_q, q_out,
+                  rope, (const int32_t *)nullptr, rows.total, 1);
 }
 template <int DH, typename T>
 cudaError_t read_t(Launch L, const Kv4Cache &c, int layer0, int layers, const Kv4Rows &rows, Kv4Tensor k, Kv4Tensor v, long long k_layer, long long v_layer) {
@@ -373,6 +410,14 @@ template <int DH> cudaError_t move_t(Launch L, const Kv4Cache &c, int B, const K
 cudaError_t kv4_append(Launch L, int dh, int dtype, const Kv4Cache &c, size_t layer_off, const Kv4Rows &rows, const Kv4Tensor *qkv, int n_q, Kv4Tensor q_out,
                        const float *rope, const int32_t *pos, int n_pos) {
   return KV4_DISPATCH(dh, dtype, append_t, L, c, layer_off, rows, qkv, n_q, q_out, rope, pos, n_pos);
+}
+cudaError_t kv4_append_sums(Launch L, int dh, const Kv4Cache &c, size_t layer_off, const Kv4Rows &rows, SplitIn qkv, RowScale sc, int n_q, float *q_out,
+                            const float2 *rope) {
+  const int width = c.n_kv_heads * dh;
+  const FromSums src{qkv, sc, width, dh};
+  const Kv4Tensor q{q_out, width, dh};
+  const float *t = reinterpret_cast<const float *>(rope);
+  return dh == 128 ? append_sums_t<128>(L, c, layer_off, rows, src, n_q, q, t) : append_sums_t<64>(L, c, layer_off, rows, src, n_q, q, t);
 }
 cudaError_t kv4_read(Launch L, int dh, int dtype, const Kv4Cache &c, int layer0, int layers, const Kv4Rows &rows, Kv4Tensor k, Kv4Tensor v, long long k_layer,
                      long long v_layer) {

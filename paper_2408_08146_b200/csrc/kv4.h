@@ -16,6 +16,9 @@ struct Kv4Moves {
 // qkv: q, k, v; q rotated to q_out where n_q > 0.  rope: [n_pos][dh/2] (cos, sin) or null; pos: row of it (null: the slot).
 cudaError_t kv4_append(Launch L, int dh, int dtype, const Kv4Cache &c, size_t layer_off, const Kv4Rows &rows, const Kv4Tensor *qkv, int n_q, Kv4Tensor q_out,
                        const float *rope, const int32_t *pos, int n_pos);
+// The same from the partial sums of a Q/K/V multiply (as many query heads as kv heads, n_q of them wanted: 0 or all); row r of the rope table is row r's.
+cudaError_t kv4_append_sums(Launch L, int dh, const Kv4Cache &c, size_t layer_off, const Kv4Rows &rows, SplitIn qkv, RowScale sc, int n_q, float *q_out,
+                            const float2 *rope);
 cudaError_t kv4_read(Launch L, int dh, int dtype, const Kv4Cache &c, int layer0, int layers, const Kv4Rows &rows, Kv4Tensor k, Kv4Tensor v, long long k_layer,
                      long long v_layer);
 cudaError_t kv4_move(Launch L, int dh, const Kv4Cache &c, int B, const Kv4Moves &m);

@@ -4,6 +4,12 @@
 
 using namespace koala;
 
+namespace koala {
+
+bool kv4_describe(const koala_kv4 *k, const int32_t *table, int table_stride, Kv4Cache *out);
+
+}  // namespace koala
+
 namespace {
 
 constexpr int NUM_SMS = 148;
@@ -66,6 +72,17 @@ int done(cudaError_t e) { return e == cudaSuccess ? KOALA_OK : KOALA_E_CUDA; }
 
 static_assert(KOALA_FP32 == KV4_FP32 && KOALA_BF16 == KV4_BF16 && KOALA_FP16 == KV4_FP16, "storage types");
 static_assert(KOALA_MAX_TREE == KV4_MAX_MOVES, "a tree's nodes in one call");
+
+namespace koala {
+
+// The kernels' view of a caller's cache; false: the description is invalid.
+bool kv4_describe(const koala_kv4 *k, const int32_t *table, int table_stride, Kv4Cache *out) {
+  if (!cache_ok(k) || !pages_ok(k) || table == nullptr || table_stride < 1 || (long long)table_stride * k->page_size > (1ll << 30)) return false;
+  *out = cache_of(k, table, table_stride);
+  return true;
+}
+
+}  // namespace koala
 
 extern "C" {
 #pragma GCC visibility push(default)
