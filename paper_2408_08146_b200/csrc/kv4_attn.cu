@@ -66,18 +66,35 @@ __device__ __forceinline__ uint4 lds128(uint32_t at) {
 
 // CTAs that share an SM, by registers: four warps hide too little of each other's waits with three (one sequence of 131071 slots MEASURE)
 template <int NT, bool PAIR> constexpr int CTAS = NT == 1 ? (PAIR ? 3 : 4) : 2;
-template <int NT> constexpr int DEPTH = NT == 1 ? 3 : 5;      // steps of a warp in its ring
+template <int NT, bool CLUSTER> constexpr int DEPTH = NT == 1 ? (CLUSTER ? 2 : 3) : 5;      // steps of a warp in its ring
 // Granules per step of a warp: two where registers allow, for independent instructions and half the bookkeeping.
 template <int NT> constexpr int STEP = NT == 1 ? 2 : 1;
-template <int DH, int NT> constexpr int RING = WARPS * DEPTH<NT> * STEP<NT> * kv4_granule_bytes(DH);
+template <int DH, int NT, bool CLUSTER> constexpr int RING = WARPS * DEPTH<NT, CLUSTER> * STEP<NT> * kv4_granule_bytes(DH);
+// CLUSTER: behind the ring, what the cluster's CTAs send to the one that has a row
+constexpr int PEERS = 8;
+template <int DH, int NT, bool CLUSTER> constexpr int SMEM = RING<DH, NT, CLUSTER> + (CLUSTER ? (8 * NT + PEERS) * (DH + 4) * 4 : 0);
 
-template <int DH, int NT, bool PAIR>
+// the address of the same place in the memory of CTA `rank` of the cluster
+__device__ __forceinline__ uint32_t peer_at(uint32_t local, uint32_t rank) {
+  uint32_t a;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(local), "r"(rank));
+  return a;
+}
+__device__ __forceinline__ void send(uint32_t at, float4 v) {
+  asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(at), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
+}
+__device__ __forceinline__ void send(uint32_t at, float2 v) { asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(at), "f"(v.x), "f"(v.y) : "memory"); }
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
+
+// CLUSTER: grid (CTAs of a cluster, kv heads, sequences * tiles); the cluster's CTAs share an item's granules and send their sums to one another.
+template <int DH, int NT, bool PAIR, bool CLUSTER>
 __global__ void __launch_bounds__(32 * WARPS, CTAS<NT, PAIR>) kv4_attn_kernel(const Kv4Attn A, float *__restrict__ scratch, int tiles) {
   constexpr int KS = DH / 16;              // depth steps of S
   constexpr int MT = DH / 16;              // tiles of 16 dims of O
-  constexpr int ROWS = 8 * NT, OS = DH + 4, GB = kv4_granule_bytes(DH), H = STEP<NT>, STAGES = DEPTH<NT>;
+  constexpr int ROWS = 8 * NT, OS = DH + 4, GB = kv4_granule_bytes(DH), H = STEP<NT>, STAGES = DEPTH<NT, CLUSTER>;
   extern __shared__ __align__(128) unsigned char smem[];
-  static_assert(WARPS * ROWS * OS * 4 <= RING<DH, NT>, "the warps' sums go where the ring was");
+  static_assert(WARPS * ROWS * OS * 4 <= RING<DH, NT, CLUSTER>, "the warps' sums go where the ring was");
   float *part = reinterpret_cast<float *>(smem);          // [WARPS][ROWS][OS]
   pdl_wait();
   pdl_launch_dependents();                 // in this order: the kernel that follows reads the plan before its own wait
@@ -87,10 +104,29 @@ __global__ void __launch_bounds__(32 * WARPS, CTAS<NT, PAIR>) kv4_attn_kernel(co
   const uint32_t ring = smem_at(smem) + (uint32_t)(warp * STAGES * H * GB);
 
   Walk<ROWS, 1> walk;
-  if (!walk.begin(A, tiles, G, lane, blockIdx.x == 0 && warp == 0)) return;
   Piece pc;
+  const unsigned rank = CLUSTER ? blockIdx.x : 0u, peers = CLUSTER ? gridDim.x : 1u;
+  if constexpr (CLUSTER) {
+    cluster_arrive();                      // waited for before a peer's memory is written: it has begun
+    const Item it = item_of<ROWS, 1>(A, (int)blockIdx.z, tiles, G, blockIdx.x + blockIdx.y == 0 && warp == 0);
+    if (it.span == 0) {                    // for all of the cluster
+      cluster_wait();
+      return;
+    }
+    pc.b = tiles == 1 ? (int)blockIdx.z : (int)blockIdx.z / tiles;
+    pc.hk = (int)blockIdx.y;
+    pc.row0 = ((int)blockIdx.z - pc.b * tiles) * ROWS;
+    pc.first = it.first; pc.count = it.count; pc.ctx = it.ctx; pc.kv = it.kv;
+    const unsigned granules = (unsigned)((it.kv + KV4_G - 1) / KV4_G), n = (granules + H - 1) / H;      // (n * peers < 2^31)
+    pc.lo = (int)(n * rank / peers) * H;
+    pc.hi = min((int)granules, (int)(n * (rank + 1) / peers) * H);
+    pc.begins = true;
+    pc.whole = peers == 1u;
+  } else {
+    if (!walk.begin(A, tiles, G, lane, blockIdx.x == 0 && warp == 0)) return;
+  }
 #pragma unroll 1
-  while (walk.next(A, G, lane, pc)) {
+  while (CLUSTER || walk.next(A, G, lane, pc)) {
     const int lo = pc.lo, hi = pc.hi, hk = pc.hk, row0 = pc.row0;
     const int first = pc.first, count = pc.count, ctx = pc.ctx, kv = min(pc.kv, hi * KV4_G);      // slots behind `hi` are another CTA's
     const int n_rows = count * G;
@@ -459,7 +495,10 @@ __global__ void __launch_bounds__(32 * WARPS, CTAS<NT, PAIR>) kv4_attn_kernel(co
     }
     __syncthreads();
     // ---- the warps together: a result, or a partial sum.  32 WARPS / ROWS threads a row, four dims at a time
-    float *slot = part_of<DH, ROWS>(scratch, blockIdx.x, pc.begins);
+    float *slot = CLUSTER ? nullptr : part_of<DH, ROWS>(scratch, blockIdx.x, pc.begins);
+    float *inbox = reinterpret_cast<float *>(smem + RING<DH, NT, CLUSTER>);      // [sender][rows of this CTA][OS]; row r is CTA r % peers's
+    const int own = (ROWS + (int)peers - 1) / (int)peers;
+    if constexpr (CLUSTER) cluster_wait();
     constexpr int PER = 32 * WARPS / ROWS;
     const int r = threadIdx.x / PER, sub = threadIdx.x % PER;
     if (r < min(ROWS, n_rows - row0)) {
@@ -481,9 +520,40 @@ __global__ void __launch_bounds__(32 * WARPS, CTAS<NT, PAIR>) kv4_attn_kernel(co
 #pragma unroll
         for (int w = 0; w < WARPS; ++w) add4(v, f[w], *reinterpret_cast<const float4 *>(part + (w * ROWS + r) * OS + d));
         if (pc.whole) finish(A, first, hk, G, row0 + r, d, v, sum);
+        else if constexpr (CLUSTER) send(peer_at(smem_at(inbox + ((int)rank * own + r / (int)peers) * OS + d), (unsigned)r % peers), v);
         else *reinterpret_cast<float4 *>(slot + r * PART_ROW<DH> + d) = v;
       }
-      if (!pc.whole && sub == 0) *reinterpret_cast<float2 *>(slot + r * PART_ROW<DH> + DH) = make_float2(top, sum);
+      if (!pc.whole && sub == 0) {
+        if constexpr (CLUSTER) send(peer_at(smem_at(inbox + ((int)rank * own + r / (int)peers) * OS + DH), (unsigned)r % peers), make_float2(top, sum));
+        else *reinterpret_cast<float2 *>(slot + r * PART_ROW<DH> + DH) = make_float2(top, sum);
+      }
+    }
+    if constexpr (CLUSTER) {
+      if (pc.whole) return;
+      cluster_arrive();
+      cluster_wait();
+      constexpr int LANES = DH / 4;
+      const int d = 4 * (threadIdx.x % LANES);
+      for (int j = threadIdx.x / LANES; j < own; j += 32 * WARPS / LANES) {
+        const int mine = j * (int)peers + (int)rank;
+        if (mine >= min(ROWS, n_rows - row0)) break;
+        float2 ml[PEERS];
+        float top = -INFINITY, sum = 0.f;
+#pragma unroll
+        for (int k = 0; k < PEERS; ++k) {
+          ml[k] = k < (int)peers ? *reinterpret_cast<const float2 *>(inbox + (k * own + j) * OS + DH) : make_float2(-INFINITY, 0.f);
+          top = fmaxf(top, ml[k].x);
+        }
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int k = 0; k < PEERS; ++k) {
+          const float f = share(ml[k], top);
+          sum += ml[k].x == -INFINITY ? ml[k].y : f * ml[k].y;
+          if (k < (int)peers) add4(v, f, *reinterpret_cast<const float4 *>(inbox + (k * own + j) * OS + d));
+        }
+        finish(A, first, hk, G, row0 + mine, d, v, sum);
+      }
+      return;
     }
     __syncthreads();                       // the sums are read: the ring may be filled again
   }
@@ -491,13 +561,41 @@ __global__ void __launch_bounds__(32 * WARPS, CTAS<NT, PAIR>) kv4_attn_kernel(co
 
 template <int DH, int NT, bool PAIR> cudaError_t go(Launch L, const Kv4Attn &a, int num_sms) {
   static SmemOptIn optin;
-  cudaError_t e = optin.ensure((const void *)kv4_attn_kernel<DH, NT, PAIR>, RING<DH, NT>);
+  cudaError_t e = optin.ensure((const void *)kv4_attn_kernel<DH, NT, PAIR, false>, SMEM<DH, NT, false>);
   if (e != cudaSuccess) return e;
   const int G = a.n_heads / a.c.n_kv_heads, rows = a.rows.max_rows * G, tiles = (rows + 8 * NT - 1) / (8 * NT);
   const int grid = num_sms * CTAS<NT, PAIR>;
-  e = launch_k(kv4_attn_kernel<DH, NT, PAIR>, dim3(grid), dim3(32 * WARPS), RING<DH, NT>, L.st, L.pdl, a, a.scratch, tiles);
+  e = launch_k(kv4_attn_kernel<DH, NT, PAIR, false>, dim3(grid), dim3(32 * WARPS), SMEM<DH, NT, false>, L.st, L.pdl, a, a.scratch, tiles);
   if (e != cudaSuccess) return e;
   return join<DH, 8 * NT, 1>(L, a, grid, tiles, rows, num_sms);
+}
+
+// CTAs of a cluster that takes an item, 0: the items are to be dealt evenly instead.  The host knows how many slots a page-table row names, not
+// how many are in use, so the rule goes by these.  A cluster has no second launch and no plan to work out: us by slots, clusters / dealt,
+//   1 row of 32 heads      192: 6.6 / 13.1   1024: 7.5 / 13.8   4096: 11.3 / 16.9   8192: 16.6 / 19.6   16384: 26.9 / 26.7
+//   the same, batch 32     192: 18 / 30      577: 28 / 42       1024: 39 / 55       2048: 65 / 80
+//   60 rows of 32 heads    192: 11.4 / 23.7  1024: 15.7 / 22.3  2048: 21.5 / 24.8   4096: 33.4 / 29.2
+//   the same, fp32         192: 12.5 / 24.9  1024: 19.6 / 23.6  2048: 28.8 / 25.9
+// (beyond 16 rows "dealt" is kv4_attn_tc.cu).  So up to 16 granules a warp, 32 where the items fill the machine and there is nothing to deal, 12 where a
+// granule is twice the work; with tiles of 16 rows only what is resident at once, in clusters of four (of eight not all are placed at once:
+// 16 rows of 32 heads at 577 slots 14.0 us, of four 10.0).
+template <int NT, bool PAIR> int cluster_of(const Kv4Attn &a, int num_sms) {
+  const int G = a.n_heads / a.c.n_kv_heads, tiles = (a.rows.max_rows * G + 8 * NT - 1) / (8 * NT);
+  const long long tile_rows = (long long)a.rows.B * tiles, items = tile_rows * a.c.n_kv_heads, resident = (long long)num_sms * CTAS<NT, PAIR>;
+  const long long granules = (long long)a.c.table_stride << a.c.gpp_shift;
+  if (tile_rows > 65535 || a.c.n_kv_heads > 65535 || (NT == 2 && items > resident)) return 0;
+  int n = NT == 1 ? PEERS : PEERS / 2;
+  while (n > 1 && (items * n > resident || granules <= n / 2 * WARPS * STEP<NT>)) n /= 2;
+  const int most = NT == 1 ? (2 * items * n > resident ? 32 : 16) : PAIR ? 12 : 16;
+  return granules <= (long long)n * WARPS * most ? n : 0;
+}
+template <int DH, int NT, bool PAIR> cudaError_t go_cluster(Launch L, const Kv4Attn &a, int peers) {
+  static SmemOptIn optin;
+  cudaError_t e = optin.ensure((const void *)kv4_attn_kernel<DH, NT, PAIR, true>, SMEM<DH, NT, true>);
+  if (e != cudaSuccess) return e;
+  const int G = a.n_heads / a.c.n_kv_heads, tiles = (a.rows.max_rows * G + 8 * NT - 1) / (8 * NT);
+  return launch_cluster(kv4_attn_kernel<DH, NT, PAIR, true>, dim3(peers, a.c.n_kv_heads, a.rows.B * tiles), dim3(32 * WARPS), SMEM<DH, NT, true>, L.st, L.pdl,
+                        peers, a, a.scratch, tiles);
 }
 
 }  // namespace
@@ -514,8 +612,16 @@ cudaError_t kv4_attention(Launch L, int dh, const Kv4Attn &args, int num_sms) {
   const int G = a.n_heads / a.c.n_kv_heads;
   a.g_inv = G > 1 ? div_inverse((unsigned)G) : 0ull;
   const int rows = a.rows.max_rows * G;
-  if (rows > KV4_FEW_ROWS) return kv4_attention_tc(L, dh, a, num_sms);
   const bool pair = a.q_type == KV4_FP32, wide = rows > 8;
+  const int peers = wide ? (pair ? cluster_of<2, true>(a, num_sms) : cluster_of<2, false>(a, num_sms))
+                         : (pair ? cluster_of<1, true>(a, num_sms) : cluster_of<1, false>(a, num_sms));
+  if (peers > 0) {
+#define KV4_GO(D, N) (pair ? go_cluster<D, N, true>(L, a, peers) : go_cluster<D, N, false>(L, a, peers))
+    if (dh == 128) return wide ? KV4_GO(128, 2) : KV4_GO(128, 1);
+    return wide ? KV4_GO(64, 2) : KV4_GO(64, 1);
+#undef KV4_GO
+  }
+  if (rows > KV4_FEW_ROWS) return kv4_attention_tc(L, dh, a, num_sms);
 #define KV4_GO(D, N) (pair ? go<D, N, true>(L, a, num_sms) : go<D, N, false>(L, a, num_sms))
   if (dh == 128) return wide ? KV4_GO(128, 2) : KV4_GO(128, 1);
   return wide ? KV4_GO(64, 2) : KV4_GO(64, 1);

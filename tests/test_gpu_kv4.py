@@ -18,6 +18,8 @@ def ints(a):
 class World:
     """A cache of garbage pages, a random page table, and what every slot should hold."""
 
+    more_slots = 0                                       # that a row of the page table has, without a page
+
     def __init__(self, B, layers, hk, dh, page, capacity, seed=0, first_page=0):
         self.rng = np.random.default_rng(seed)
         self.B, self.L, self.hk, self.dh, self.page, self.cap = B, layers, hk, dh, page, capacity
@@ -26,7 +28,7 @@ class World:
         self.cache = PagedKV4(layers, hk, dh, page, n, device=DEV)
         self.cache.pages.fill_(0xFF)                     # codes 15, parameters NaN
         self.table_np = (first_page + self.rng.permutation(B * per + 2)[:B * per].reshape(B, per)).astype(np.int32)
-        self.table = ints(self.table_np)
+        self.table = ints(np.pad(self.table_np, ((0, 0), (0, self.more_slots // page)), constant_values=-1))
         part = lambda w: np.full((layers, B, per * page, hk, w), np.nan, np.float32)
         self.K, self.V = [part(dh), part(1), part(1), part(dh)], [part(dh), part(1), part(1), part(dh)]
         self.gen = torch.Generator(device=DEV).manual_seed(seed)
@@ -80,6 +82,12 @@ class World:
             worst = max(worst, ref.check(out[first:first + n], *r, q.dtype, f"{what} sequence {b}"))
             first += n
         return worst
+
+
+@pytest.fixture(params=[0, 1 << 17], ids=["short_tables", "long_tables"])
+def tables(request, monkeypatch):
+    """Which kernel attends goes by the slots that a page-table row names: just those in use, or many more."""
+    monkeypatch.setattr(World, "more_slots", request.param)
 
 
 def same(got, want, what):
@@ -247,10 +255,15 @@ ATTENTION = [
     (6, 2, 64, 32, [129], [31], "fp32", True),
     (4, 4, 64, 64, [1000], [40], "fp16", False),
     (1, 1, 64, 16, [0, 63, 64, 65], [17, 17, 1, 64], "fp32", False),
+    (64, 64, 128, 16, [30, 2, 70, 0, 17, 90, 64, 1, 33, 5] * 4, [1] * 40, "bf16", False),      # more items than are resident at once
+    (16, 8, 128, 16, [127] * 9 + [3], [8] * 10, "fp16", True),
+    (2, 2, 128, 16, [250], [16], "fp32", True),                                               # every size of a cluster
+    (2, 2, 64, 16, [100], [3], "bf16", True),
 ]
 
 
 @pytest.mark.parametrize("hq,hk,dh,page,ctx,count,dtype,tree", ATTENTION)
+@pytest.mark.usefixtures("tables")
 def test_attention(hq, hk, dh, page, ctx, count, dtype, tree):
     t = TYPES[dtype]
     w = World(len(ctx), 1, hk, dh, page, max(a + n for a, n in zip(ctx, count)))
@@ -277,6 +290,7 @@ def test_attention(hq, hk, dh, page, ctx, count, dtype, tree):
 
 
 @pytest.mark.parametrize("hq,hk,dh,n", [(2, 2, 128, 5), (8, 1, 64, 3), (2, 2, 128, 40), (4, 1, 128, 100)])
+@pytest.mark.usefixtures("tables")
 def test_masks_that_leave_nothing(hq, hk, dh, n):
     """No context and an empty mask: 0.  Slots that a row does not see may hold NaN and infinities."""
     w = World(2, 1, hk, dh, 16, 160)
@@ -308,6 +322,7 @@ def test_masks_that_leave_nothing(hq, hk, dh, n):
         assert torch.isnan(other[0]).all() and torch.equal(other[1:], out[1:])
 
 
+@pytest.mark.usefixtures("tables")
 def test_lengths_and_unused_rows():
     """kv_len cuts a sequence (to nothing as well); rows with a negative slot give 0; rows behind the last sequence stay."""
     w = World(3, 1, 2, 128, 16, 80)
@@ -332,6 +347,7 @@ def test_lengths_and_unused_rows():
 
 
 @pytest.mark.parametrize("hq,hk,dh,rows", [(1, 1, 128, 1), (4, 1, 64, 1), (2, 2, 128, 24)])
+@pytest.mark.usefixtures("tables")
 def test_scores_and_scales_that_grow(hq, hk, dh, rows):
     """Keys whose scores rise along the context and values whose scale jumps by 2^40: references are raised on the way."""
     n = 900
@@ -355,6 +371,7 @@ def test_scores_and_scales_that_grow(hq, hk, dh, rows):
     w.check_attention(0, q, out, [n], [rows], dh ** -0.5, what="falling")
 
 
+@pytest.mark.usefixtures("tables")
 def test_extreme_queries_and_scale():
     w = World(1, 1, 1, 128, 16, 70)
     w.fill([70])
@@ -421,6 +438,7 @@ def test_moves(dh, page, n):
     same(after[1, 3], gk[0].view(3, cap, 2, dh)[1, 0].cpu().numpy(), "moved")
 
 
+@pytest.mark.usefixtures("tables")
 def test_the_calls_together_as_a_step_of_decoding():
     """Prompt, tree, acceptance, next token: what a serving loop runs, on two layers, against the definition."""
     B, hq, hk, dh = 2, 8, 4, 128
@@ -461,6 +479,7 @@ def test_the_calls_together_as_a_step_of_decoding():
 
 
 @pytest.mark.parametrize("hq,hk,rows", [(4, 4, 1), (4, 4, 30), (2, 1, 1)])
+@pytest.mark.usefixtures("tables")
 def test_captured_and_replayed_and_on_another_stream(hq, hk, rows):
     """A step captured into graphs gives the eager bits, with new data in the same buffers; two graphs share a plan; another stream."""
     w = World(2, 1, hk, 128, 64, 4000)
