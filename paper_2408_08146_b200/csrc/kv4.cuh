@@ -45,8 +45,11 @@ struct Kv4Cache {
   // offset of granule g of sequence b and kv head h, or a negative number if the table gives no page
   template <int DH> __device__ __forceinline__ long long granule(int page, int h, int g) const {
     if ((unsigned)page >= (unsigned)n_pages) return -1;
-    const unsigned n = ((unsigned)(page * n_kv_heads + h) << gpp_shift) + (unsigned)(g & ((1 << gpp_shift) - 1));      // (below 2^31: the host's check)
-    return (long long)((unsigned long long)n * (unsigned)kv4_granule_bytes(DH));
+    return (long long)((unsigned long long)number(page, h, g) * (unsigned)kv4_granule_bytes(DH));
+  }
+  // which of the layer's granules that is, for a page that exists (below 2^31: the host's check)
+  __device__ __forceinline__ unsigned number(int page, int h, int g) const {
+    return ((unsigned)(page * n_kv_heads + h) << gpp_shift) + (unsigned)(g & ((1 << gpp_shift) - 1));
   }
   __device__ __forceinline__ int page_of(int b, int g) const {
     const int i = g >> gpp_shift;

@@ -134,37 +134,40 @@ __global__ void __launch_bounds__(32 * WARPS, CTAS<NT, PAIR>) kv4_attn_kernel(co
 
     // ---- this warp's steps of H granules: the warp-th, the one WARPS further, ..; the pages of 32 granules at a time
     const int steps = hi - lo > H * warp ? (hi - lo - H * warp + H * WARPS - 1) / (H * WARPS) : 0;
-    const unsigned char *base = A.c.pages + A.layer_off;
+    const unsigned char *base = A.c.pages + A.layer_off + lane * 16;
+    const uint32_t ring_at = ring + (uint32_t)lane * 16u;
     auto granule_of = [&](int n) { return lo + ((n / H) * WARPS + warp) * H + n % H; };      // the warp's n-th granule
-    auto pages_from = [&](int n) {
+    // a lane each looks up where the next 32 granules lie: their numbers in the layer, -1 without a page
+    auto places_from = [&](int n) {
       const int gi = granule_of(n + lane);
       if (gi >= hi) return -1;
       const int page = A.c.page_of(cache_row, gi);
-      if ((unsigned)page >= (unsigned)A.c.n_pages) A.rows.report();
-      return page;
+      if ((unsigned)page >= (unsigned)A.c.n_pages) {
+        A.rows.report();
+        return -1;
+      }
+      return (int)A.c.number(page, hk, gi);
     };
     // bit h of have[stage]: granule h of the step in that stage is there
-    int page_now = pages_from(0), page_next = pages_from(32);
+    int now = places_from(0), next = places_from(32);
     unsigned have = 0u;                    // two bits a step, the latest lowest
-    auto request = [&](int step) {         // in step order
+    auto request = [&](int step, int stage) {         // in step order
       if (step < steps) {
 #pragma unroll
         for (int h = 0; h < H; ++h) {
-          const int n = step * H + h, gi = granule_of(n);
-          const int page = __shfl_sync(0xffffffffu, page_now, n & 31);
-          const bool ok = (unsigned)page < (unsigned)A.c.n_pages;
-          have = have << 1 | (ok ? 1u : 0u);
-          if (ok) {
-            const uint32_t dst = ring + (uint32_t)((step % STAGES * H + h) * GB + lane * 16);
-            const unsigned char *src = base + A.c.granule<DH>(page, hk, gi) + lane * 16;
+          const int at = __shfl_sync(0xffffffffu, now, (step * H + h) & 31);
+          have = have << 1 | (at >= 0 ? 1u : 0u);
+          if (at >= 0) {
+            const uint32_t dst = ring_at + (uint32_t)((stage * H + h) * GB);
+            const unsigned char *src = base + (long long)at * GB;
 #pragma unroll
             for (int i = 0; i < GB / 512; ++i) copy16(dst + i * 512, src + i * 512);
             if (lane < (GB % 512) / 16) copy16(dst + GB / 512 * 512, src + GB / 512 * 512);
           }
-          if ((n & 31) == 31) {            // the next 32 granules' pages
-            page_now = page_next;
-            page_next = pages_from(n + 33);
-          }
+        }
+        if ((step * H & 31) == 32 - H) {   // the next 32 granules
+          now = next;
+          next = places_from(step * H + H + 32);
         }
       } else {
         have <<= H;
@@ -172,7 +175,7 @@ __global__ void __launch_bounds__(32 * WARPS, CTAS<NT, PAIR>) kv4_attn_kernel(co
       asm volatile("cp.async.commit_group;" ::: "memory");
     };
 #pragma unroll
-    for (int i = 0; i < STAGES - 1; ++i) request(i);
+    for (int i = 0; i < STAGES - 1; ++i) request(i, i);
 
     // ---- row g as a column of operand B (q), rows 2t and 2t + 1 as columns of the scores
     uint32_t qf[PAIR ? 2 : 1][NT][KS][2];
@@ -253,15 +256,17 @@ __global__ void __launch_bounds__(32 * WARPS, CTAS<NT, PAIR>) kv4_attn_kernel(co
     }
     float C = pow2i(100);                  // power of two on the V scales, lowered as larger ones come
 
+    int stage = 0;
 #pragma unroll 1
     for (int step = 0; step < steps; ++step) {
       __syncwarp();                        // the stage asked for now was read in the previous step
-      request(step + STAGES - 1);
+      request(step + STAGES - 1, stage == 0 ? STAGES - 1 : stage - 1);
       asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1) : "memory");
       __syncwarp();
       const unsigned there = have >> ((STAGES - 1) * H) & ((1u << H) - 1u);      // bit H - 1 - h: granule h
+      const uint32_t at = ring + (uint32_t)(stage * H * GB);
+      stage = stage + 1 == STAGES ? 0 : stage + 1;
       if (there == 0u) continue;
-      const uint32_t at = ring + (uint32_t)(step % STAGES * H * GB);
       const int key0 = granule_of(step * H) * KV4_G;
       // ---- S^T
       float s[H][NT][4];
