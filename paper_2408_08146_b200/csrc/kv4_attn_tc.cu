@@ -53,7 +53,9 @@ template <int DH> struct Lay {
   static constexpr int K = 0, V = NB * ONE, CODES = 2 * NB * ONE;
   static constexpr int PART = kv4_granule_bytes(DH);
   static constexpr int Q = CODES + EXPANDERS * RING * PART;  // rows of queries as they come: 128 of 16 bits, or 64 of 32
-  static constexpr int BYTES = Q + 128 * DH * 2;
+  // the results on their way out, 32 dims of a warp's rows at a time: where the warp's own queries came in, or where these are too short behind them
+  static constexpr int OUT = DH == 128 ? Q : Q + 128 * DH * 2;
+  static constexpr int BYTES = OUT + 32768;
 };
 template <int DH> constexpr unsigned SMEM = Lay<DH>::BYTES + 1024;
 
@@ -736,8 +738,10 @@ __global__ void __launch_bounds__(THREADS, 1) kv4_attn_tc_kernel(const Kv4Attn A
         zs = (f0 != 0.f ? f0 * x0.w : 0.f) + (f1 != 0.f ? f1 * x1.w : 0.f);
       }
       const float inv = !pc.whole ? 1.f : ml.y != 0.f && (used || !in) ? 1.f / ml.y : 0.f;      // nothing seen, or not in use: 0
-      float *part = part_of<DH, ROWS>(scratch, blockIdx.x, pc.begins) + row * PART_ROW<DH>;
-      const long long out = in ? (long long)(pc.first + i_row) * A.out.row + (long long)(pc.hk * G + rr - i_row * G) * A.out.head : 0;
+      float *part = part_of<DH, ROWS>(scratch, blockIdx.x, pc.begins);
+      const int r_own = MODE == FULL ? lane : lane & 15;
+      // (DH 128: both groups are done with the queries that came in here, and only this warp writes them)
+      const uint32_t stage = sb + LY::OUT + (uint32_t)(DH == 128 ? (quarter * 2 + group) * (MODE == HALF ? 2048 : 4096) : warp * 4096);
       unit[0] *= inv;
       unit[1] *= inv;
       zs *= inv;
@@ -750,33 +754,49 @@ __global__ void __launch_bounds__(THREADS, 1) kv4_attn_tc_kernel(const Kv4Attn A
           tmem_ld16(mine + (uint32_t)(COL_O + k * O_COLS + c + 16), o[k] + 16);
         }
         wait_ld();
+        // columns 8w + 2i + k: dim 4 (c / 8 + w) + i of half k.  Through shared memory, place p of a row's eight at p ^ (row & 7)
+        auto sum = [&](int j) {
+          float x = 0.f;
 #pragma unroll
-        for (int j = 0; j < 32; ++j) {
-          float x = zs;
+          for (int k = 0; k < 2; ++k)
+            if (unit[k] != 0.f) x = fmaf(__uint_as_float(o[k][j]), unit[k], x);      // (an O that was never written may hold anything)
+          return x;
+        };
 #pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            float a = __uint_as_float(o[k][j]);
-            if (MODE != FULL) a += __shfl_xor_sync(0xffffffffu, a, 16);
-            if (unit[k] != 0.f) x = fmaf(a, unit[k], x);         // (an O that was never written may hold anything)
-          }
-          o[0][j] = __float_as_uint(x);
-        }
-        if (in) {
+        for (int w = 0; w < 4; ++w) {
+          float x[2][4];
 #pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            auto even = [&](int k) { return make_float4(__uint_as_float(o[0][8 * w + k]), __uint_as_float(o[0][8 * w + 2 + k]), __uint_as_float(o[0][8 * w + 4 + k]), __uint_as_float(o[0][8 * w + 6 + k])); };
-            const int d = 4 * (c / 8 + w);
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-              if (MODE != FULL && k != half) continue;
-              if (pc.whole) store_out(A, out + d + k * (DH / 2), even(k));
-              else *reinterpret_cast<float4 *>(part + d + k * (DH / 2)) = even(k);
+          for (int i = 0; i < 4; ++i) {
+            const float a = sum(8 * w + 2 * i), b = sum(8 * w + 2 * i + 1);
+            if constexpr (MODE == FULL) {
+              x[0][i] = a + zs;
+              x[1][i] = b + zs;
+            } else {                       // the row's other lane has the other keys' part: this one takes the dims of its own half
+              x[0][i] = (half ? b : a) + __shfl_xor_sync(0xffffffffu, half ? a : b, 16) + zs;
             }
+          }
+#pragma unroll
+          for (int k = 0; k < (MODE == FULL ? 2 : 1); ++k)
+            sts128(stage + (uint32_t)(r_own * 128 + (((4 * (MODE == FULL ? k : half) + w) ^ (r_own & 7)) << 4)), __float_as_uint(x[k][0]), __float_as_uint(x[k][1]),
+                   __float_as_uint(x[k][2]), __float_as_uint(x[k][3]));
+        }
+        __syncwarp();
+#pragma unroll 4
+        for (int k = lane; k < ROWS / 4 * 8; k += 32) {
+          const int r = k >> 3, place = k & 7, at = quarter * (ROWS / 4) + r, d = 4 * (c / 8 + (place & 3)) + (place >> 2) * (DH / 2);
+          const uint4 raw = lds128(stage + (uint32_t)(r * 128 + ((place ^ (r & 7)) << 4)));
+          const float4 v = make_float4(__uint_as_float(raw.x), __uint_as_float(raw.y), __uint_as_float(raw.z), __uint_as_float(raw.w));
+          if (pc.row0 + at >= n_rows) continue;
+          if (pc.whole) {
+            const int i = A.by_group(pc.row0 + at);
+            store_out(A, (long long)(pc.first + i) * A.out.row + (long long)(pc.hk * G + pc.row0 + at - i * G) * A.out.head + d, v);
+          } else {
+            *reinterpret_cast<float4 *>(part + at * PART_ROW<DH> + d) = v;
           }
         }
         __syncwarp();
       }
-      if (!pc.whole && in && half == 0 && group == 0) *reinterpret_cast<float2 *>(part + DH) = ml;
+      if (!pc.whole && in && half == 0 && group == 0) *reinterpret_cast<float2 *>(part + row * PART_ROW<DH> + DH) = ml;
       fence_before();
       __syncwarp();
       if (n > 0 && lane == 0) arrive(&sync.x_empty);
