@@ -29,6 +29,7 @@ template <typename T> __device__ __forceinline__ void store4(T *p, const float *
 
 // Where the new rows come from: the caller's tensors, or the partial sums of the Q/K/V multiply.
 template <typename T> struct FromTensors {
+  static constexpr int AT_ONCE = 2;
   Kv4Tensor q, k, v;
   // what a thread needs of the vectors `which` (q, k, v) of head h from element c on
   struct Column {
@@ -48,6 +49,7 @@ template <typename T> struct FromTensors {
 
 // The partial sums of the Q/K/V multiply: columns q | k | v of `width` each, every row with a scale owed by the norm before.
 struct FromSums {
+  static constexpr int AT_ONCE = 1;            // rows whose loads are on their way together: as many as registers allow
   SplitIn s;
   RowScale sc;
   int width, dh;
@@ -86,46 +88,56 @@ __device__ __forceinline__ void rotate4(float *a, float *b, const float *cs) {
 }
 
 // a / b rounded to nearest, for b's reciprocal y rounded to nearest: the quotient a y is off by an ulp at most, its remainder is exact, and adding
-// remainder times y rounds correctly (Markstein, IBM J. Res. Dev. 34, 1990), as long as nothing leaves the range of normal numbers; here
-// 2^-100 <= b < 2^125, and where the remainder does, a / b is below 2^-20 and its code 0.
-__device__ __forceinline__ float quotient(float a, float b, float y) {
-  const float q = __fmul_rn(a, y);
-  return __fmaf_rn(__fmaf_rn(-b, q, a), y, q);
+// remainder times y rounds correctly (Markstein, IBM J. Res. Dev. 34, 1990), as long as nothing leaves the range of normal numbers.  For the
+// codes 2^-100 <= b < 2^125, and where the remainder leaves it, a / b is below 2^-20 and the code 0; for the scale b is 15, and where it
+// does, the scale is far below 2^-100.  (An infinite a gives a NaN.)  Two quotients at a time: half the instructions, which are the bound.
+__device__ __forceinline__ f32x2 quotients(f32x2 a, f32x2 minus_b, f32x2 y) {
+  const f32x2 q = mul2(a, y);
+  return fma2(fma2(minus_b, q, a), y, q);
+}
+// NaN if one of them is
+__device__ __forceinline__ float min3(float a, float b, float c) {
+  float d;
+  asm("min.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
 }
 
 // Codes of this lane's eight numbers as a word, and the vector's parameters (scale in the low half).
 // A code needs no clamp: zero <= x, and x - zero <= 15 scale (1 + 2^-23).  Its rounding to a whole number is the addition of 1.5 * 2^23,
-// after which it stands in the low bits; the upper bits' constant is taken off the word once.
+// after which it stands in the low bits; the upper bits' constant is taken off the word once.  A NaN anywhere makes both ends NaN, an infinity
+// makes the range infinite or NaN: either way the scale is not finite.
 template <int DH> __device__ __forceinline__ uint32_t quantise(const float *a, const float *b, uint32_t &params) {
   constexpr int LPV = DH / 8;
-  float lo = a[0], hi = a[0], odd = 0.f;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    lo = fminf(lo, fminf(a[i], b[i]));
-    hi = fmaxf(hi, fmaxf(a[i], b[i]));
-    odd = fmaf(b[i], 0.f, fmaf(a[i], 0.f, odd));            // NaN where something is not finite
-  }
+  float lo = min3(min3(a[0], a[1], a[2]), min3(a[3], b[0], b[1]), min3(b[2], b[3], b[3]));
+  float hi = max3(max3(a[0], a[1], a[2]), max3(a[3], b[0], b[1]), max3(b[2], b[3], b[3]));
 #pragma unroll
   for (int o = LPV / 2; o > 0; o >>= 1) {
-    lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-    hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+    const float l2 = __shfl_xor_sync(0xffffffffu, lo, o), h2 = __shfl_xor_sync(0xffffffffu, hi, o);
+    lo = min3(lo, l2, l2);
+    hi = max3(hi, h2, h2);
   }
-  const unsigned group = (LPV == 16 ? 0xffffu : 0xffu) << ((threadIdx.x & 31) / LPV * LPV);
   const bf16 z = __float2bfloat16_rd(lo);
-  const float zero = __bfloat162float(z);
-  bf16 s = __float2bfloat16_ru(__fdiv_rn(__fsub_rn(hi, zero), 15.f));
+  const float zero = __bfloat162float(z), fifteenth = 1.f / 15.f;
+  bf16 s = __float2bfloat16_ru(apart(quotients(both(__fsub_rn(hi, zero), 0.f), both(-15.f, -15.f), both(fifteenth, fifteenth))).x);
   const float scale = __bfloat162float(s);
-  const bool bad = (__ballot_sync(0xffffffffu, odd != 0.f) & group) != 0u || !(scale < INFINITY);
+  const bool bad = !(scale < INFINITY);
   const bool flat = scale < 7.888609052210118e-31f;       // 2^-100
   if (flat) s = __float2bfloat16_rn(0.f);
   params = bad ? 0x7fff7fffu : (uint32_t)__bfloat16_as_ushort(s) | (uint32_t)__bfloat16_as_ushort(z) << 16;
   if (flat || bad) return 0u;
   const float y = __frcp_rn(scale);
+  const f32x2 y2 = both(y, y), minus = both(-scale, -scale), from = both(-zero, -zero), whole = both(12582912.f, 12582912.f);
   uint32_t w = 0u;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    w += __float_as_uint(quotient(__fsub_rn(a[i], zero), scale, y) + 12582912.f) << (4 * i);
-    w += __float_as_uint(quotient(__fsub_rn(b[i], zero), scale, y) + 12582912.f) << (16 + 4 * i);
+    const float2 c = apart(add2(quotients(add2(both(a[i], b[i]), from), minus, y2), whole));
+    w += __float_as_uint(c.x) << (4 * i);
+    w += __float_as_uint(c.y) << (16 + 4 * i);
   }
   return w - 0x4b400000u * 0x1111u - (0x4b400000u << 16) * 0x1111u;
 }
@@ -139,7 +151,7 @@ constexpr int BLOCK_ROWS = 16, ROWS_AT_ONCE = 4;
 template <int DH, bool MANY, typename Src, typename TQ>
 __global__ void __launch_bounds__(256, MANY ? 4 : 1) kv4_append_kernel(Kv4Cache c, size_t layer_off, Kv4Rows rows, Src src, int n_q, Kv4Tensor q_out,
                                                          const float *rope, const int32_t *pos, int n_pos, int by_row) {
-  constexpr int LPV = DH / 8, RB = MANY ? BLOCK_ROWS : 1, AT = MANY ? ROWS_AT_ONCE / 2 : 1;
+  constexpr int LPV = DH / 8, RB = MANY ? BLOCK_ROWS : 1, AT = MANY ? Src::AT_ONCE : 1;
   pdl_launch_dependents();
   pdl_wait();
   rows.check();
@@ -150,7 +162,7 @@ __global__ void __launch_bounds__(256, MANY ? 4 : 1) kv4_append_kernel(Kv4Cache 
   const int h = which == 0 ? vec : which == 1 ? vec - n_q : vec - n_q - c.n_kv_heads;
   // lane j: row r0 + j
   Kv4Place mine{-1, -1, 0, 0, 0};
-  int turn = 0;
+  int turn = 0, granule = -1;   // granule: of kv head 0
   if (lane < RB) {
     mine = kv4_place(c, rows, r0 + lane);
     turn = by_row ? r0 + lane : pos != nullptr && mine.page >= 0 ? pos[r0 + lane] : mine.slot;
@@ -158,6 +170,7 @@ __global__ void __launch_bounds__(256, MANY ? 4 : 1) kv4_append_kernel(Kv4Cache 
       rows.report();
       mine.page = -1;
     }
+    if (mine.page >= 0) granule = (int)c.number(mine.page, 0, mine.slot >> 4);
   }
   unsigned shadowed = 0u;       // bit j: a later row of the sequence has row j's slot: that one is kept
   if (rows.slot != nullptr)
@@ -169,7 +182,7 @@ __global__ void __launch_bounds__(256, MANY ? 4 : 1) kv4_append_kernel(Kv4Cache 
       if (__any_sync(0xffffffffu, again)) shadowed |= 1u << j;
     }
   const bool any_kv = __any_sync(0xffffffffu, which != 0);       // warps of nothing but queries have nothing to quantise
-  unsigned char *base = c.pages + layer_off;
+  unsigned char *base = c.pages + layer_off + ((long long)(which == 0 ? 0 : h) << c.gpp_shift) * kv4_granule_bytes(DH);
   const auto column = src.column(live ? which : 1, live ? h : 0, 4 * l);
   TQ *const to_q = which == 0 ? reinterpret_cast<TQ *>(q_out.p) + (long long)h * q_out.head + 4 * l : nullptr;
   const float *const turns = rope == nullptr || which == 2 ? nullptr : rope + 8 * l;
@@ -177,13 +190,13 @@ __global__ void __launch_bounds__(256, MANY ? 4 : 1) kv4_append_kernel(Kv4Cache 
   for (int j0 = 0; j0 < RB; j0 += AT) {
     float a[AT][4], e[AT][4];
     float4 cs[AT][2];
-    int page[AT], slot[AT];
+    int at[AT], slot[AT];
 #pragma unroll
     for (int k = 0; k < AT; ++k) {
-      page[k] = __shfl_sync(0xffffffffu, mine.page, j0 + k);
+      at[k] = __shfl_sync(0xffffffffu, granule, j0 + k);
       slot[k] = __shfl_sync(0xffffffffu, mine.slot, j0 + k);
       const int p = __shfl_sync(0xffffffffu, turn, j0 + k);
-      const bool use = live && page[k] >= 0;
+      const bool use = live && at[k] >= 0;
 #pragma unroll
       for (int x = 0; x < 4; ++x) a[k][x] = e[k][x] = 0.f;
       if (use) column.load(r0 + j0 + k, a[k], e[k], DH / 2);
@@ -197,7 +210,7 @@ __global__ void __launch_bounds__(256, MANY ? 4 : 1) kv4_append_kernel(Kv4Cache 
     }
 #pragma unroll
     for (int k = 0; k < AT; ++k) {
-      if (page[k] < 0) continue;           // (the same for the whole block)
+      if (at[k] < 0) continue;             // (the same for the whole block)
       const int r = r0 + j0 + k;
       if (turns != nullptr) rotate4(a[k], e[k], &cs[k][0].x);
       if (live && which == 0) {
@@ -209,7 +222,7 @@ __global__ void __launch_bounds__(256, MANY ? 4 : 1) kv4_append_kernel(Kv4Cache 
       uint32_t params;
       const uint32_t w = quantise<DH>(a[k], e[k], params);       // (whole warps: the vectors of a warp may be of both kinds)
       if (live && which != 0 && (shadowed >> (j0 + k) & 1u) == 0u) {
-        unsigned char *g = base + c.granule<DH>(page[k], h, slot[k] >> 4);
+        unsigned char *g = base + (long long)at[k] * kv4_granule_bytes(DH);
         const int s = slot[k] & 15;
         *reinterpret_cast<uint32_t *>(g + (which == 1 ? kv4_k_at<DH>(s, l) : kv4_v_at<DH>(s, l))) = w;
         if (l == 0) *reinterpret_cast<uint32_t *>(g + kv4_p_at<DH>(s, which - 1)) = params;
