@@ -1,6 +1,8 @@
 // Writing, moving and reading rows of the paged 4-bit cache (kv4.cuh has the format).
 #include <cuda_fp16.h>
 
+#include <type_traits>
+
 #include "kv4.h"
 
 namespace koala {
@@ -29,7 +31,6 @@ template <typename T> __device__ __forceinline__ void store4(T *p, const float *
 
 // Where the new rows come from: the caller's tensors, or the partial sums of the Q/K/V multiply.
 template <typename T> struct FromTensors {
-  static constexpr int AT_ONCE = 2;
   Kv4Tensor q, k, v;
   // what a thread needs of the vectors `which` (q, k, v) of head h from element c on
   struct Column {
@@ -49,7 +50,6 @@ template <typename T> struct FromTensors {
 
 // The partial sums of the Q/K/V multiply: columns q | k | v of `width` each, every row with a scale owed by the norm before.
 struct FromSums {
-  static constexpr int AT_ONCE = 1;            // rows whose loads are on their way together: as many as registers allow
   SplitIn s;
   RowScale sc;
   int width, dh;
@@ -142,16 +142,19 @@ template <int DH> __device__ __forceinline__ uint32_t quantise(const float *a, c
   return w - 0x4b400000u * 0x1111u - (0x4b400000u << 16) * 0x1111u;
 }
 
-// Rows of a block: their places are looked up by a lane each, which takes four dependent loads (3 us of the 3.6 us that a block with one
-// row takes), and the loads of ROWS_AT_ONCE rows are on their way together.  One row where that leaves SMs without a block.
-constexpr int BLOCK_ROWS = 16, ROWS_AT_ONCE = 4;
+// Rows of a block: their places are looked up by a lane each, four dependent loads.  One row where that leaves SMs without a block.
+// Appending waits for these, for its rows and for chains of few instructions, so warps count for more than rows at once in a warp: with reading
+// back 8192 rows of 32 + 8 + 8 heads take 66 us with 8 rows a block, one at a time, 48 warps an SM; 69 us with 16 rows; 73 us with two
+// at a time and 32 warps.  Reading has eight rows on their way together (2047 rows of 8 layers: 16 rows a block 83 us, 8 rows 90 us).
+constexpr int BLOCK_ROWS = 8, READ_ROWS = 16;
+template <typename Src> constexpr int CTAS = std::is_same<Src, FromSums>::value ? 4 : 6;
 
 // grid (blocks of rows, groups of vectors): a block takes 256 * 8 / DH of the rows' n_q + 2 n_kv vectors.
-// Bound: bytes (append_prompt MEASURE).  MANY: BLOCK_ROWS rows a block, else one.
+// Bound: what it waits for; 16384 rows of 8 + 8 heads 40 us (2.1 TB/s), with 32 query heads turned 93 us (3.8 TB/s).  MANY: BLOCK_ROWS rows a block, else one.
 template <int DH, bool MANY, typename Src, typename TQ>
-__global__ void __launch_bounds__(256, MANY ? 4 : 1) kv4_append_kernel(Kv4Cache c, size_t layer_off, Kv4Rows rows, Src src, int n_q, Kv4Tensor q_out,
+__global__ void __launch_bounds__(256, MANY ? CTAS<Src> : 1) kv4_append_kernel(Kv4Cache c, size_t layer_off, Kv4Rows rows, Src src, int n_q, Kv4Tensor q_out,
                                                          const float *rope, const int32_t *pos, int n_pos, int by_row) {
-  constexpr int LPV = DH / 8, RB = MANY ? BLOCK_ROWS : 1, AT = MANY ? Src::AT_ONCE : 1;
+  constexpr int LPV = DH / 8, RB = MANY ? BLOCK_ROWS : 1;
   pdl_launch_dependents();
   pdl_wait();
   rows.check();
@@ -187,46 +190,33 @@ __global__ void __launch_bounds__(256, MANY ? 4 : 1) kv4_append_kernel(Kv4Cache 
   TQ *const to_q = which == 0 ? reinterpret_cast<TQ *>(q_out.p) + (long long)h * q_out.head + 4 * l : nullptr;
   const float *const turns = rope == nullptr || which == 2 ? nullptr : rope + 8 * l;
 #pragma unroll 1
-  for (int j0 = 0; j0 < RB; j0 += AT) {
-    float a[AT][4], e[AT][4];
-    float4 cs[AT][2];
-    int at[AT], slot[AT];
-#pragma unroll
-    for (int k = 0; k < AT; ++k) {
-      at[k] = __shfl_sync(0xffffffffu, granule, j0 + k);
-      slot[k] = __shfl_sync(0xffffffffu, mine.slot, j0 + k);
-      const int p = __shfl_sync(0xffffffffu, turn, j0 + k);
-      const bool use = live && at[k] >= 0;
-#pragma unroll
-      for (int x = 0; x < 4; ++x) a[k][x] = e[k][x] = 0.f;
-      if (use) column.load(r0 + j0 + k, a[k], e[k], DH / 2);
-      if (turns != nullptr && use) {
-        const float4 *t = reinterpret_cast<const float4 *>(turns + (size_t)p * DH);
-        cs[k][0] = t[0];
-        cs[k][1] = t[1];
-      } else {
-        cs[k][0] = cs[k][1] = make_float4(1.f, 0.f, 1.f, 0.f);
-      }
+  for (int j = 0; j < RB; ++j) {
+    const int at = __shfl_sync(0xffffffffu, granule, j), s = __shfl_sync(0xffffffffu, mine.slot, j) & 15, p = __shfl_sync(0xffffffffu, turn, j);
+    const int r = r0 + j;
+    float a[4] = {0.f, 0.f, 0.f, 0.f}, e[4] = {0.f, 0.f, 0.f, 0.f};
+    float4 cs[2];
+    if (live && at >= 0) column.load(r, a, e, DH / 2);
+    if (turns != nullptr && live && at >= 0) {            // (not where it is used: all loads of a row are on their way together)
+      const float4 *t = reinterpret_cast<const float4 *>(turns + (size_t)p * DH);
+      cs[0] = t[0];
+      cs[1] = t[1];
+    } else {
+      cs[0] = cs[1] = make_float4(1.f, 0.f, 1.f, 0.f);
     }
-#pragma unroll
-    for (int k = 0; k < AT; ++k) {
-      if (at[k] < 0) continue;             // (the same for the whole block)
-      const int r = r0 + j0 + k;
-      if (turns != nullptr) rotate4(a[k], e[k], &cs[k][0].x);
-      if (live && which == 0) {
-        TQ *o = to_q + r * q_out.row;
-        store4(o, a[k]);
-        store4(o + DH / 2, e[k]);
-      }
-      if (!any_kv) continue;
-      uint32_t params;
-      const uint32_t w = quantise<DH>(a[k], e[k], params);       // (whole warps: the vectors of a warp may be of both kinds)
-      if (live && which != 0 && (shadowed >> (j0 + k) & 1u) == 0u) {
-        unsigned char *g = base + (long long)at[k] * kv4_granule_bytes(DH);
-        const int s = slot[k] & 15;
-        *reinterpret_cast<uint32_t *>(g + (which == 1 ? kv4_k_at<DH>(s, l) : kv4_v_at<DH>(s, l))) = w;
-        if (l == 0) *reinterpret_cast<uint32_t *>(g + kv4_p_at<DH>(s, which - 1)) = params;
-      }
+    if (at < 0) continue;                  // (the same for the whole block)
+    if (turns != nullptr) rotate4(a, e, &cs[0].x);
+    if (live && which == 0) {
+      TQ *o = to_q + r * q_out.row;
+      store4(o, a);
+      store4(o + DH / 2, e);
+    }
+    if (!any_kv) continue;
+    uint32_t params;
+    const uint32_t w = quantise<DH>(a, e, params);        // (whole warps: the vectors of a warp may be of both kinds)
+    if (live && which != 0 && (shadowed >> j & 1u) == 0u) {
+      unsigned char *g = base + (long long)at * kv4_granule_bytes(DH);
+      *reinterpret_cast<uint32_t *>(g + (which == 1 ? kv4_k_at<DH>(s, l) : kv4_v_at<DH>(s, l))) = w;
+      if (l == 0) *reinterpret_cast<uint32_t *>(g + kv4_p_at<DH>(s, which - 1)) = params;
     }
   }
 }
@@ -235,7 +225,7 @@ __global__ void __launch_bounds__(256, MANY ? 4 : 1) kv4_append_kernel(Kv4Cache 
 template <int DH, bool MANY, typename T>
 __global__ void __launch_bounds__(256) kv4_read_kernel(Kv4Cache c, int layer0, Kv4Rows rows, Kv4Tensor k_out, Kv4Tensor v_out, long long k_layer,
                                                        long long v_layer) {
-  constexpr int LPV = DH / 8, RB = MANY ? BLOCK_ROWS : 1, AT = MANY ? 2 * ROWS_AT_ONCE : 1;
+  constexpr int LPV = DH / 8, RB = MANY ? READ_ROWS : 1, AT = MANY ? 8 : 1;
   pdl_launch_dependents();
   pdl_wait();
   rows.check();
@@ -371,8 +361,8 @@ __global__ void __launch_bounds__(32 * MOVE_WARPS) kv4_move_kernel(Kv4Cache c, K
 }
 
 constexpr int NUM_SMS = 148;
-// BLOCK_ROWS rows a block only where that still gives every SM a block
-bool many_rows(int total, int slices) { return (long long)((total + BLOCK_ROWS - 1) / BLOCK_ROWS) * slices >= 2 * NUM_SMS; }
+// `rows` of them a block only where that still gives every SM two blocks
+bool many_rows(int total, int slices, int rows) { return (long long)((total + rows - 1) / rows) * slices >= 2 * NUM_SMS; }
 
 template <int DH, typename T>
 cudaError_t append_t(Launch L, const Kv4Cache &c, size_t layer_off, const Kv4Rows &rows, const Kv4Tensor *x, int n_q, Kv4Tensor q_out, const float *rope,
@@ -380,7 +370,7 @@ cudaError_t append_t(Launch L, const Kv4Cache &c, size_t layer_off, const Kv4Row
   const int per = 256 * 8 / DH, n_vec = n_q + 2 * c.n_kv_heads;
   const FromTensors<T> src{x[0], x[1], x[2]};
   const int slices = (n_vec + per - 1) / per;
-  if (many_rows(rows.total, slices))
+  if (many_rows(rows.total, slices, BLOCK_ROWS))
     return launch_k(kv4_append_kernel<DH, true, FromTensors<T>, T>, dim3((rows.total + BLOCK_ROWS - 1) / BLOCK_ROWS, slices), dim3(256), 0, L.st, L.pdl, c,
                     layer_off, rows, src, n_q, q_out, rope, pos, n_pos, 0);
   return launch_k(kv4_append_kernel<DH, false, FromTensors<T>, T>, dim3(rows.total, slices), dim3(256), 0, L.st, L.pdl, c, layer_off, rows, src, n_q, q_out,
@@ -389,7 +379,7 @@ cudaError_t append_t(Launch L, const Kv4Cache &c, size_t layer_off, const Kv4Row
 template <int DH>
 cudaError_t append_sums_t(Launch L, const Kv4Cache &c, size_t layer_off, const Kv4Rows &rows, const FromSums &src, int n_q, Kv4Tensor q_out, const float *rope) {
   const int per = 256 * 8 / DH, slices = (n_q + 2 * c.n_kv_heads + per - 1) / per;
-  if (many_rows(rows.total, slices))
+  if (many_rows(rows.total, slices, BLOCK_ROWS))
     return launch_k(kv4_append_kernel<DH, true, FromSums, float>, dim3((rows.total + BLOCK_ROWS - 1) / BLOCK_ROWS, slices), dim3(256), 0, L.st, L.pdl, c,
                     layer_off, rows, src, n_q, q_out, rope, (const int32_t *)nullptr, rows.total, 1);
   return launch_k(kv4_append_kernel<DH, false, FromSums, float>, dim3(rows.total, slices), dim3(256), 0, L.st, L.pdl, c, layer_off, rows, src, n_q, q_out,
@@ -398,8 +388,8 @@ cudaError_t append_sums_t(Launch L, const Kv4Cache &c, size_t layer_off, const K
 template <int DH, typename T>
 cudaError_t read_t(Launch L, const Kv4Cache &c, int layer0, int layers, const Kv4Rows &rows, Kv4Tensor k, Kv4Tensor v, long long k_layer, long long v_layer) {
   const int per = 256 * 8 / DH, slices = (2 * c.n_kv_heads + per - 1) / per;
-  if (many_rows(rows.total, slices * layers))
-    return launch_k(kv4_read_kernel<DH, true, T>, dim3((rows.total + BLOCK_ROWS - 1) / BLOCK_ROWS, slices, layers), dim3(256), 0, L.st, L.pdl, c, layer0, rows,
+  if (many_rows(rows.total, slices * layers, READ_ROWS))
+    return launch_k(kv4_read_kernel<DH, true, T>, dim3((rows.total + READ_ROWS - 1) / READ_ROWS, slices, layers), dim3(256), 0, L.st, L.pdl, c, layer0, rows,
                     k, v, k_layer, v_layer);
   return launch_k(kv4_read_kernel<DH, false, T>, dim3(rows.total, slices, layers), dim3(256), 0, L.st, L.pdl, c, layer0, rows, k, v, k_layer, v_layer);
 }
