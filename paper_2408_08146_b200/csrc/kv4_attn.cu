@@ -12,7 +12,9 @@
 // factor or the final scale, exactly.  For V the codes are centred first (one fp16 subtraction of 8 per two codes, exact): the
 // tensor core adds by truncation, about 2e-8 of the sum per multiply, and without it the sum carries 7.5 times the sum of the
 // weights, hundreds of times the result where many slots average out (131071 slots: 2e-3 off instead of 3e-4).  With fp32
-// queries a granule's product starts from zero and is added to the sum in registers, rounded.
+// queries all codes come centred and as normal numbers (see centred(); subnormal ones left 3e-6 of an error where plain fp32 has
+// 5e-7, normal ones 3e-7, and take 9% longer where the rows are few), and a granule's product starts from zero and is added to the sum in
+// registers, rounded.
 // Rounding: q enters as fp16, each row first scaled by a power of two to a maximum of 2^14 .. 2^15 (bf16 and fp16 queries
 // lose nothing down to 2^-29 of the row's maximum); fp32 queries as two fp16 values (22 bits).  A weight p_j scaleV_j
 // enters as one fp16 value scaled by a power of two (11 bits: relative error 2^-12, as much as the rounding of an fp16
@@ -54,6 +56,13 @@ __device__ __forceinline__ uint32_t add2(uint32_t a, uint32_t b) {
   return *reinterpret_cast<const uint32_t *>(&h);
 }
 
+// Codes in bits 0 .. 3, or 4 .. 7, of either half as code - 8, or 16 (code - 8), exactly.  NORMAL: put under the exponent of 1024, and that taken off
+// again; else 2^-24 times that, by one addition.  The tensor core lines products up by the exponents of their factors and cuts off what lies 24
+// bits or so below the largest, and a subnormal factor counts with the exponent of 2^-14 however small it is: numbers below 16 * 2^-24
+// lose six to ten bits that way.
+template <bool NORMAL> __device__ __forceinline__ uint32_t centred(uint32_t codes) { return NORMAL ? add2(codes | 0x64006400u, 0xe408e408u) : add2(codes, 0x80088008u); }
+template <bool NORMAL> __device__ __forceinline__ uint32_t centred16(uint32_t codes) { return NORMAL ? add2(codes | 0x64006400u, 0xe480e480u) : add2(codes, 0x80808080u); }
+
 __device__ __forceinline__ uint32_t smem_at(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ void copy16(uint32_t dst, const void *src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
@@ -91,6 +100,7 @@ __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.w
 template <int DH, int NT, bool PAIR, bool CLUSTER>
 __global__ void __launch_bounds__(32 * WARPS, CTAS<NT, PAIR>) kv4_attn_kernel(const Kv4Attn A, float *__restrict__ scratch, int tiles) {
   constexpr int KS = DH / 16;              // depth steps of S
+  constexpr float UNIT = PAIR ? 1.f : 16777216.f;      // 1 / what a code counts
   constexpr int MT = DH / 16;              // tiles of 16 dims of O
   constexpr int ROWS = 8 * NT, OS = DH + 4, GB = kv4_granule_bytes(DH), H = STEP<NT>, STAGES = DEPTH<NT, CLUSTER>;
   extern __shared__ __align__(128) unsigned char smem[];
@@ -238,7 +248,7 @@ __global__ void __launch_bounds__(32 * WARPS, CTAS<NT, PAIR>) kv4_attn_kernel(co
           }
         }
       const float scale = A.scale * 1.4426950408889634f;
-      const float f = fminf(scale * 16777216.f / up, 3e38f), z = sum * (up * 5.9604644775390625e-8f);
+      const float f = fminf(scale * UNIT / up, 3e38f), z = sum * (up / UNIT);
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         F[n][j] = __shfl_sync(0xffffffffu, f, (2 * t + j) * 4);
@@ -295,8 +305,8 @@ __global__ void __launch_bounds__(32 * WARPS, CTAS<NT, PAIR>) kv4_attn_kernel(co
               const uint32_t x = e == 0 ? kx[h][w] : kx[h][w] >> 8, y = e == 0 ? ky[h][w] : ky[h][w] >> 8;
               uint32_t a[4] = {x & 0x000f000fu, y & 0x000f000fu, x & 0x00f000f0u, y & 0x00f000f0u};
               if constexpr (PAIR) {
-                a[0] = add2(a[0], 0x80088008u); a[1] = add2(a[1], 0x80088008u);
-                a[2] = add2(a[2], 0x80808080u); a[3] = add2(a[3], 0x80808080u);
+                a[0] = centred<true>(a[0]); a[1] = centred<true>(a[1]);
+                a[2] = centred16<true>(a[2]); a[3] = centred16<true>(a[3]);
               }
 #pragma unroll
               for (int n = 0; n < NT; ++n) {
@@ -448,8 +458,10 @@ __global__ void __launch_bounds__(32 * WARPS, CTAS<NT, PAIR>) kv4_attn_kernel(co
           uint32_t y = __byte_perm(b0, b1, 0x5410), yh = __byte_perm(b0, b1, 0x7632);
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const uint32_t mask = (i & 1) ? 0x00f000f0u : 0x000f000fu, eight = (i & 1) ? 0x80808080u : 0x80088008u;      // -8 * 16, -8
-            const uint32_t a[4] = {add2(x & mask, eight), add2(xh & mask, eight), add2(y & mask, eight), add2(yh & mask, eight)};
+            const uint32_t mask = (i & 1) ? 0x00f000f0u : 0x000f000fu;
+            uint32_t a[4] = {x & mask, xh & mask, y & mask, yh & mask};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) a[k] = (i & 1) ? centred16<PAIR>(a[k]) : centred<PAIR>(a[k]);
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
               if constexpr (PAIR) {
@@ -485,7 +497,7 @@ __global__ void __launch_bounds__(32 * WARPS, CTAS<NT, PAIR>) kv4_attn_kernel(co
 #pragma unroll
         for (int w = 0; w < DH / 64; ++w) {
           const int d = 4 * (g * (DH / 64) + w);
-          const float f[2] = {16777216.f * back, 1048576.f * back};      // 2^24, less the 16 of the upper nibbles
+          const float f[2] = {UNIT * back, 0.0625f * UNIT * back};       // the upper nibbles came 16 times as large
           float x[4], y[4];
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
