@@ -167,6 +167,31 @@ def test_odd_vectors():
         assert np.isnan(w.K[3][0, 0, 3 + 8, 0]).all() and not np.isnan(w.K[3][0, 0, 3 + 8, 1]).any()
 
 
+@pytest.mark.parametrize("dh", [64, 128])
+def test_codes_and_scales_are_those_of_a_division(dh):
+    """Ranges of every size, and numbers half way between two codes or next to it: the kernel's quotients round as a division does."""
+    n, hk = 1500, 3
+    w = World(1, 1, hk, dh, 64, n)
+    rng = np.random.default_rng(dh)
+    size = np.exp2(rng.uniform(-98, 120, (2, n, hk, 1)))
+    x = (rng.uniform(-1, 1, (2, n, hk, dh)) * size + rng.uniform(-4, 4, (2, n, hk, 1)) * size * (rng.random((2, n, hk, 1)) < 0.5)).astype(np.float32)
+    # the second half: half-way numbers of the vector's own grid, moved by up to two units in the last place; the ends stay
+    _, zero, scale, _ = ref.quantise(x[:, n // 2:])
+    half = (zero + scale * (rng.integers(0, 15, x[:, n // 2:].shape) + np.float32(0.5))).astype(np.float32)
+    half = np.where(half == 0, half, (half.view(np.int32) + rng.integers(-2, 3, half.shape).astype(np.int32)).view(np.float32))
+    lo, hi = x[:, n // 2:].min(-1, keepdims=True), x[:, n // 2:].max(-1, keepdims=True)
+    half = np.clip(half, lo, hi)
+    half[..., :1], half[..., 1:2] = lo, hi
+    x[:, n // 2:] = half
+    k, v = (torch.from_numpy(np.ascontiguousarray(t)).to(DEV) for t in x)
+    rows = w.plan([0], [n])
+    w.cache.append(0, rows, k, v)
+    w.put(0, np.zeros(n, int), np.arange(n), x[0], x[1])
+    gk, gv = w.cache.read(rows, layer=0, dtype=torch.float32)
+    same(gk, w.K[3][0, 0, :n], "keys")
+    same(gv, w.V[3][0, 0, :n], "values")
+
+
 def test_slots_of_their_own():
     """Rows at given slots: negative ones are left out, of two with the same slot the last one is kept."""
     w = World(2, 1, 2, 128, 16, 64)

@@ -107,6 +107,34 @@ def test_scratch_of_the_attention():
     assert lib.koala_kv4_attention(C.byref(cache_c()), 0, C.byref(rows_c(max_rows=1 << 20, total=1, row_start=4096)), 1, tensors(GOOD, GOOD), 4, 0.1, 4096, 1 << 40, None) == UNSUPPORTED
 
 
+def test_more_work_than_is_counted():
+    """Units of work are counted in 32 bits."""
+    for c, r in ((cache_c(n_kv_heads=1), rows_c(B=60000, total=60000, table_stride=1 << 26)),
+                 (cache_c(n_kv_heads=1), rows_c(B=1, total=1 << 30, max_rows=1 << 30)),
+                 (cache_c(n_kv_heads=8), rows_c(B=8000, total=8000 * 128, max_rows=128, table_stride=1 << 18))):      # 64000 heads, 2 tiles, 65544 units
+        assert attention(c, r, heads=c.n_kv_heads) == UNSUPPORTED
+        assert int(m._library().koala_kv4_attention_scratch_bytes(C.byref(c), C.byref(r), c.n_kv_heads)) == 0
+    # as many sequences of as many slots are fine one by one
+    assert attention(cache_c(n_kv_heads=1), rows_c(B=60000, total=60000, table_stride=16), heads=1) == CAPACITY       # (no scratch)
+    assert attention(cache_c(n_kv_heads=1), rows_c(B=1, total=1, table_stride=1 << 26), heads=1) == CAPACITY
+
+
+def test_rows_belong_to_caches_of_one_shape():
+    memory = torch.zeros(1 << 16, dtype=torch.uint8)
+    memory = memory[-memory.data_ptr() % 128:]
+    make = lambda **kw: PagedKV4(**{**dict(n_layers=1, n_kv_heads=2, head_dim=64, page_size=16, n_pages=4, device="cpu", pages=memory), **kw})
+    table, ctx = torch.zeros(1, 4, dtype=torch.int32), torch.zeros(1, dtype=torch.int32)
+    rows = make().rows(table, ctx)
+    for other in (make(n_kv_heads=4), make(head_dim=128), make(page_size=32)):
+        shape = torch.zeros(1, other.n_kv_heads, other.head_dim)
+        with pytest.raises(ValueError):
+            other.append(0, rows, shape, shape)
+        with pytest.raises(ValueError):
+            other.attention(0, rows, shape)
+        with pytest.raises(ValueError):
+            other.read(rows)
+
+
 def test_the_binding_checks_its_tensors():
     with pytest.raises(KoalaError):
         PagedKV4(1, 2, 100, 16, 4, device="cpu")
