@@ -341,7 +341,7 @@ typedef struct {
 /* The cache of a context made with KOALA_F_KV4: n_layers = L, n_kv_heads = n_heads, head_dim as the configuration; page_table
  * (DEVICE [B][table_stride]) names pages for at least S_max slots a sequence, entries that are not reached yet may be anything.  *cache is
  * copied; pages and table are borrowed.  To be called before the first forward, and again whenever the table or the pages
- * have moved, between koala_accept and the next call.  The contents of the table may change between calls: they are read when kernels run.
+ * have moved, but not between koala_verify and koala_accept (KOALA_E_STATE).  The contents of the table may change between calls: they are read when kernels run.
  * A slot without a page sets the device status to KOALA_E_INVALID. */
 int koala_set_kv4(koala_ctx *ctx, const koala_kv4 *cache, const int32_t *page_table, int32_t table_stride);
 
@@ -349,10 +349,10 @@ int koala_set_kv4(koala_ctx *ctx, const koala_kv4 *cache, const int32_t *page_ta
  * DEVICE arrays; made once, it serves every layer of the forward. */
 typedef struct {
   uint32_t struct_size;      /* sizeof(koala_kv4_rows) */
-  int32_t B;
+  int32_t B;                 /* B * n_kv_heads <= 65535 */
   int32_t total;             /* rows of the call's tensors */
   int32_t max_rows;          /* host-known bound on the rows of one sequence; <= 128 with `slot` or `mask` */
-  int32_t table_stride;
+  int32_t table_stride;      /* table_stride * page_size <= 2^30.  Few slots a row of the table let the attention take its short form */
   const int32_t *page_table; /* [B][table_stride]: page of slots page_size * i .. ; anything outside 0 .. n_pages-1: none */
   const int32_t *ctx_len;    /* [B] slots held before these rows: row i of a sequence lies at slot ctx_len + i */
   const int32_t *row_start;  /* [B+1] rows row_start[b] .. row_start[b+1]-1 belong to sequence b; NULL: max_rows rows each.
@@ -384,7 +384,10 @@ int koala_kv4_append(const koala_kv4 *cache, int32_t layer, const koala_kv4_rows
 /* out = softmax(scale * q K^T) V over the slots that each row sees: those below ctx_len, and behind them by `mask` or order, below
  * kv_len.  A row that sees nothing, or is not in use, gives 0.  Heads h of q share kv head h / (n_heads / n_kv_heads).  t: HOST array
  * of two tensors of `dtype` [total][n_heads]: q and out (which may be q).  scratch: device, 16-byte aligned, >=
- * koala_kv4_attention_scratch_bytes() (which may be 0), not shared by calls that may overlap.  Accumulation and softmax in fp32. */
+ * koala_kv4_attention_scratch_bytes() (0: nothing to do, or refused), not shared by calls that may overlap.  Accumulation and softmax in fp32;
+ * codes enter the multiplies as they are, q with its leading 11 bits (bf16 and fp16 exactly; fp32: 22) and the weights with 11 (fp32: 22).
+ * KOALA_E_UNSUPPORTED: more than 2^19 (row, head) pairs of one sequence and kv head, or more work than is counted in 32 bits: for each
+ * sequence, kv head and 64 such pairs a unit per 64 slots (up to 16 pairs: per 16 slots) that a page-table row could name. */
 size_t koala_kv4_attention_scratch_bytes(const koala_kv4 *cache, const koala_kv4_rows *rows, int32_t n_heads);
 int koala_kv4_attention(const koala_kv4 *cache, int32_t layer, const koala_kv4_rows *rows, int32_t dtype,
                         const koala_kv4_tensor *t, int32_t n_heads, float scale, void *scratch, size_t scratch_bytes,

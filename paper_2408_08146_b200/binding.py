@@ -277,6 +277,9 @@ class Koala:
         if cache.device != self.dev:
             raise ValueError(f"the cache is on {cache.device}")
         self._check(self.lib.koala_set_kv4(self._ctx, cache._p, page_table.data_ptr(), page_table.size(1)))
+        for t in (cache.pages, page_table):     # they may be another stream's, and be let go of while kernels are under way
+            if t.is_cuda:
+                t.record_stream(self.stream)
         self.kv4 = (cache, page_table)
 
     def koala_draft(self, p: int):

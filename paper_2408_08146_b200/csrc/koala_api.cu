@@ -823,7 +823,9 @@ int draft_eagle(koala_ctx *c, int pass) {
 int compact(koala_ctx *c) {
   const koala_config &g = c->cfg;
   if (c->kv4) {
-    const Kv4Moves m{c->pend_cap, g.N, c->t.acc_path, nullptr, c->t.acc_S, c->t.acc_len, c->status};      // no path is longer than pend_cap
+    // No path is longer than pend_cap.  kv_len is the verification's: 0 for a tree that did not fit and was not written, whose slots may have no
+    // page of the sequence's own.  (Behind an ingestion it is its blocks'; the path is a chain then, and nothing moves.)
+    const Kv4Moves m{c->pend_cap, g.N, c->t.acc_path, nullptr, c->t.acc_S, c->t.acc_len, row_plan(c).kv_len, c->status};
     CU_TRY(kv4_move(LN(c), g.head_dim, c->kv4_cache, g.B, m));
   }
   CU_TRY(kv_compact(LN(c), g.dtype, c->t, c->verify_hid, c->tk, c->tv, c->kv4 ? 0 : g.L, g.B, g.N, g.n_heads, g.head_dim, g.S_max));
@@ -1074,6 +1076,7 @@ int koala_set_kv4(koala_ctx *c, const koala_kv4 *cache, const int32_t *page_tabl
   if (!c) return KOALA_E_INVALID;
   const koala_config &g = c->cfg;
   if (!c->kv4) return fail(c, KOALA_E_STATE, "the context was not made with KOALA_F_KV4");
+  if (c->phase == PH_VERIFIED) return fail(c, KOALA_E_STATE, "the tree's keys and values are in the cache that koala_accept is to move them in");
   Kv4Cache view;
   if (!kv4_describe(cache, page_table, table_stride, &view)) return fail(c, KOALA_E_INVALID, "bad description of the 4-bit cache");
   if (cache->n_layers != g.L || cache->n_kv_heads != g.n_heads || cache->head_dim != g.head_dim)

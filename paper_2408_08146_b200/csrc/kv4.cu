@@ -286,8 +286,9 @@ __global__ void __launch_bounds__(32 * MOVE_WARPS) kv4_move_kernel(Kv4Cache c, K
   const int S = m.base != nullptr ? m.base[b] : 0;
   for (int i = threadIdx.x; i < n; i += blockDim.x) {
     int src = m.src[(size_t)b * m.stride + i], dst = m.dst != nullptr ? m.dst[(size_t)b * m.stride + i] : i;
-    const bool used = src >= 0 && dst >= 0;
+    bool used = src >= 0 && dst >= 0;
     if (used) { src += S; dst += S; }
+    if (m.kv_len != nullptr) used = used && max(src, dst) < m.kv_len[b];
     long long f = -1, t = -1;
     if (used && src != dst) {
       f = c.granule<DH>(c.page_of(b, src >> 4), 0, src >> 4);

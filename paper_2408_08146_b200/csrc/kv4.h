@@ -10,6 +10,7 @@ struct Kv4Moves {
   int stride;
   const int32_t *src, *dst;                     // [B][stride]; entries with a negative one are left out; dst null: 0, 1, ..
   const int32_t *base, *count;                  // [B] added to both; how many of the n are used (null: 0; n)
+  const int32_t *kv_len;                        // [B] slots in use: nothing is moved to or from behind them (null: anywhere)
   int *status;
 };
 

@@ -146,7 +146,7 @@ int koala_kv4_move(const koala_kv4 *k, int32_t B, const int32_t *page_table, int
   if ((long long)table_stride * k->page_size > (1ll << 30)) return KOALA_E_INVALID;
   if (n > KV4_MAX_MOVES || (long long)k->n_layers * k->n_kv_heads > (1 << 30)) return KOALA_E_UNSUPPORTED;
   if (n == 0) return KOALA_OK;
-  const Kv4Moves m{n, n, src, dst, nullptr, nullptr, status};
+  const Kv4Moves m{n, n, src, dst, nullptr, nullptr, nullptr, status};
   return done(kv4_move(Launch{(cudaStream_t)cuda_stream, true}, k->head_dim, cache_of(k, page_table, table_stride), B, m));
 }
 

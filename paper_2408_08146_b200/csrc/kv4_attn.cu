@@ -1,11 +1,13 @@
 // Attention of a few query rows over the paged 4-bit cache (kv4.cuh has the format), on mma.sync.
 //
-// One CTA = (key chunk, tile of 8 NT query rows, kv head of a sequence); a query row is a (token, head) pair of the heads that
-// share the kv head.  Its warps take the chunk's granules of 16 slots in turn.  With x = zero + scale * code
+// An item is a tile of 8 NT query rows of one kv head and sequence; a query row is a (token, head) pair of the heads that
+// share the kv head.  A CTA has some of an item's granules of 16 slots, which its warps take in turn, each through a ring of its own in shared
+// memory (cp.async).  Either a cluster has the item, its CTAs a share each, and sends the sums to the CTA that finishes a row; or all items stand
+// in a line that is dealt evenly (kv4_work.cuh), and a second kernel joins the parts.  With x = zero + scale * code
 //   q . K_j        = scaleK_j (q . codeK_j) + zeroK_j sum(q)
 //   sum_j p_j V_j  = sum_j (p_j scaleV_j) codeV_j + sum_j p_j zeroV_j
-// so the multiplies take bare codes and nothing is expanded in memory: a warp loads a granule straight into the registers
-// of operand A (16 bytes per lane and load, the cache's order), S^T = K Q^T with slots as rows, then O^T += V^T P^T with
+// so the multiplies take bare codes and nothing is expanded in memory: a granule comes as it lies in the cache, in the order of
+// the registers of operand A (16 bytes per lane and load), S^T = K Q^T with slots as rows, then O^T += V^T P^T with
 // dims as rows; P^T changes from accumulator to operand layout by an 8x8 transposition of registers.
 // A code 0..15 in the low bits of an fp16 IS that number times 2^-24 (subnormal), and in bits 4..7 16 times that: masking a
 // word gives two operands without any conversion.  The factors 2^-24 and 16 are powers of two and go into q, the row's
@@ -21,6 +23,10 @@
 // result, an eighth of a bf16 one); with fp32 queries as two.  Everything else is fp32.
 // The softmax is online with a reference maximum that is raised only when a score exceeds it by more than 2^4: in the common
 // case a granule needs no shuffles but one vote.
+// Bound: issue slots.  A granule of 8 rows takes a warp some 300 instructions, half of them to take codes out of words, and four warps on a
+// scheduler issue 0.54 of the time (one sequence of 131071 slots, 8 kv heads: 40.3 us, 3.5 TB/s of the 6.55 that a copy reaches; DRAM 46%, the
+// tensor pipe 22%, the integer pipe 47% of their time).  Tried against it and no faster: codes centred by a second multiply instead of an
+// addition (41.6 us), two granules at a time with tiles of 16 rows, deeper rings.
 #include "kv4_work.cuh"
 
 namespace koala {
@@ -73,7 +79,8 @@ __device__ __forceinline__ uint4 lds128(uint32_t at) {
   return v;
 }
 
-// CTAs that share an SM, by registers: four warps hide too little of each other's waits with three (one sequence of 131071 slots MEASURE)
+// CTAs that share an SM, by registers: as many as there can be (32 ragged sequences up to 8190 slots: 55.3 us with four, 59.1 with three; one of
+// 131071 slots, where three keep their registers: 40.2 and 38.7)
 template <int NT, bool PAIR> constexpr int CTAS = NT == 1 ? (PAIR ? 3 : 4) : 2;
 template <int NT, bool CLUSTER> constexpr int DEPTH = NT == 1 ? (CLUSTER ? 2 : 3) : 5;      // steps of a warp in its ring
 // Granules per step of a warp: two where registers allow, for independent instructions and half the bookkeeping.

@@ -174,7 +174,7 @@ __device__ __forceinline__ void finish(const Kv4Attn &A, int first, int hk, int 
 }
 
 // Joins the parts of the items that lie in several CTAs.  grid (items, blocks of `per` rows), or, where there are more items than CTAs, (CTAs, ..): the one
-// item that begins in that CTA and goes on behind it.  A block takes 3 us even when it finds nothing to do, so few of them, two a SM
+// item that begins in that CTA and goes on behind it.  Blocks come and go at a cost even when they find nothing to do, so few of them, two a SM
 // at most where the rows allow.  For each row as many groups of DH / 4 threads as there are, which take its parts in turn, BATCH at a time
 // on their way together.
 constexpr int JOIN_THREADS = 512;

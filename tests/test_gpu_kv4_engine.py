@@ -176,7 +176,10 @@ def test_moved_pages_and_a_new_table():
     tok, parent = p.tree(30)
     tok[0] = p.orc.root_tok[0]
     p.verify([(tok, parent)])
+    with pytest.raises(KoalaError):                      # the tree lies in these pages
+        p.eng.set_kv4(moved, table)
     p.accept([3])
+    p.eng.set_kv4(moved, table)
     p.finish()
 
 
@@ -221,4 +224,27 @@ def test_a_slot_without_a_page_is_reported():
         eng.prefill([np.arange(20)], 60)
         if eng.device_status() != 0:
             raise KoalaError(eng.device_status(), "reported")
+    eng.close()
+
+
+def test_a_tree_that_does_not_fit_moves_nothing():
+    """100 + 60 nodes in 128 slots: reported, and no page changes, whatever the table says about slots that are not reached."""
+    cfg = reduced(T7_EAGLE, 1, K=1, V=256, S_max=128, prompt_len=16)
+    cache = PagedKV4(1, cfg.n_heads, cfg.head_dim, 16, 16, device=DEV)
+    cache.pages.zero_()
+    table = torch.arange(8, dtype=torch.int32, device=DEV).view(1, 8)
+    table[0, 7] = 0                                      # slots 112 .. : the first page once more
+    eng = Koala(cfg, WeightStore(cfg, DEV).tensors, kv4=(cache, table))
+    eng.prefill([np.arange(100)], 60)
+    assert eng.device_status() == 0
+    before = cache.pages.clone()
+    tok = torch.zeros(1, 60, dtype=torch.int32, device=DEV)
+    parent = torch.zeros(1, 60, dtype=torch.int32, device=DEV)
+    parent[0, 0], parent[0, 20], parent[0, 21:] = -1, 1, torch.arange(20, 59, device=DEV)      # the walk: 0, 1, 20, 21, which would lie at slots 100 ..
+    n = torch.full((1,), 60, dtype=torch.int32, device=DEV)
+    eng.koala_verify((tok, parent, n, 60))
+    eng.koala_accept(torch.tensor([4], dtype=torch.int32, device=DEV))
+    torch.cuda.synchronize()
+    assert torch.equal(cache.pages, before)
+    assert eng.device_status() == 3                      # KOALA_E_CAPACITY
     eng.close()
