@@ -111,6 +111,7 @@ __global__ void __launch_bounds__(32 * WARPS, CTAS<NT, PAIR>) kv4_attn_kernel(co
   constexpr int MT = DH / 16;              // tiles of 16 dims of O
   constexpr int ROWS = 8 * NT, OS = DH + 4, GB = kv4_granule_bytes(DH), H = STEP<NT>, STAGES = DEPTH<NT, CLUSTER>;
   extern __shared__ __align__(128) unsigned char smem[];
+  __shared__ Plan plan;                    // (CLUSTER: not used)
   static_assert(WARPS * ROWS * OS * 4 <= RING<DH, NT, CLUSTER>, "the warps' sums go where the ring was");
   float *part = reinterpret_cast<float *>(smem);          // [WARPS][ROWS][OS]
   pdl_wait();
@@ -140,7 +141,9 @@ __global__ void __launch_bounds__(32 * WARPS, CTAS<NT, PAIR>) kv4_attn_kernel(co
     pc.begins = true;
     pc.whole = peers == 1u;
   } else {
-    if (!walk.begin(A, tiles, G, lane, blockIdx.x == 0 && warp == 0)) return;
+    if (warp == 0) plan_for<ROWS, 1>(A, tiles, G, lane, blockIdx.x == 0, plan);
+    __syncthreads();
+    walk.begin(plan, tiles);
   }
 #pragma unroll 1
   while (CLUSTER || walk.next(A, G, lane, pc)) {

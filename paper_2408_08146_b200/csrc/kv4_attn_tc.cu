@@ -71,6 +71,7 @@ struct alignas(16) Sync {
   int error;
   TileInfo info[INFO];
   float2 q_stat[128];                      // largest magnitude and sum of each row of queries
+  Plan plan;
   float4 x[2][128];                        // the groups' maximum, sum and power of two of each row
 };
 
@@ -186,6 +187,8 @@ __global__ void __launch_bounds__(THREADS, 1) kv4_attn_tc_kernel(const Kv4Attn A
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sync.tmem)), "r"((uint32_t)TMEM_COLS) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
+  // (while the allocation waits for the launch before to free its own)
+  if (warp == PV_WARP + 1) plan_for<ROWS, UG>(A, tiles, G, lane, blockIdx.x == 0, sync.plan);
   fence_before();
   __syncthreads();
   fence_after();
@@ -193,7 +196,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv4_attn_tc_kernel(const Kv4Attn A
   pdl_launch_dependents();                 // after the allocation: what follows may want tensor memory too; and after the wait: the joining kernel reads the plan early
 
   Walk<ROWS, UG> walk;
-  bool more = walk.begin(A, tiles, G, lane, blockIdx.x == 0 && warp == 0);
+  walk.begin(sync.plan, tiles);
   Piece pc;
   int tt = 0;                              // tiles before this piece (of this CTA)
   bool ok = true;
@@ -223,7 +226,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv4_attn_tc_kernel(const Kv4Attn A
     const int ps = lane & 15;
     const bool pv = lane >= 16;
     const uint32_t p_from = (uint32_t)(KV4_G * DH + (ps & 7) * 16 + (pv ? 8 : 0) + (ps >> 3) * 4);
-    while (more && ok && walk.next(A, G, lane, pc)) {
+    while (ok && walk.next(A, G, lane, pc)) {
       const int n = pc.hi - pc.lo, kv = min(pc.kv, pc.hi * TK), cache_row = A.rows.cache_of(pc.b);
       uint64_t or0 = ~0ull, or1 = ~0ull;   // slots behind ctx that some row sees
       if (tree && pc.hi * TK > pc.ctx) {
@@ -368,7 +371,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv4_attn_tc_kernel(const Kv4Attn A
     const uint32_t leader = lane == 0 ? 1u : 0u, tm = __shfl_sync(0xffffffffu, tmem, 0);
     int tile = 0, buf = 0;                 // tiles issued, and the buffer of the next
     uint32_t phase = 0u, q_phase = 0u;
-    while (warp <= PV_WARP && more && ok && walk.next(A, G, lane, pc)) {
+    while (warp <= PV_WARP && ok && walk.next(A, G, lane, pc)) {
       const int n = __shfl_sync(0xffffffffu, pc.hi - pc.lo, 0);
       if (warp == S_WARP && n > 0) {
         const uint32_t idesc = (1u << 4) | ((uint32_t)(TK >> 3) << 17) | ((128u >> 4) << 24);                             // fp32, fp16 x fp16, N = 64
@@ -413,7 +416,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv4_attn_tc_kernel(const Kv4Attn A
     const uint32_t mine = tmem + ((uint32_t)(quarter * 32) << 16), o_at = mine + (uint32_t)(COL_O + group * O_COLS);
     const float log2_scale = A.scale * 1.4426950408889634f;
     int pieces = 0;
-    while (more && ok && walk.next(A, G, lane, pc)) {
+    while (ok && walk.next(A, G, lane, pc)) {
       const int n = pc.hi - pc.lo, kv = min(pc.kv, pc.hi * TK);
       const int rr = pc.row0 + row, n_rows = pc.count * G, i_row = A.by_group(rr);
       const bool in = rr < n_rows;

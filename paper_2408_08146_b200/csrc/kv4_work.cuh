@@ -63,61 +63,95 @@ template <int ROWS, int UG> __device__ __forceinline__ unsigned cta_count(unsign
   return n < grid ? n : grid;
 }
 
-// A CTA's run of units, item by item; whole warps walk through it together.
+// A piece of a CTA's run of units; whole warps walk through the run together, item by item.
 struct Piece {
   int b, hk, row0, first, count, ctx, kv, lo, hi;     // keys: units lo .. hi - 1, of those the slots below kv
   bool begins, whole;                                 // the item's first unit is this CTA's; all of them are
 };
-template <int ROWS, int UG> struct Walk {
+// One warp works out where the CTA's run begins and ends, and writes the items down where there are at most 32 tiles of sequences, so that
+// the others need neither loads nor sums (four 64-row trees: 47.7 us with every warp looking for itself, 45.6 us so).
+struct Plan {
+  Item item[32];
+  unsigned upto[32];                                  // units up to and with each
   unsigned u, end;
-  int entries, tiles;
-  // false: nothing to do for this CTA
-  __device__ __forceinline__ bool begin(const Kv4Attn &A, int n_tiles, int G, int lane, bool tell) {
-    tiles = n_tiles;
-    entries = A.rows.B * tiles;
-    const unsigned Hk = (unsigned)A.c.n_kv_heads;
-    unsigned U = 0;
-    for (int j = 0; j < entries; j += 32) U += (unsigned)item_of<ROWS, UG>(A, j + lane, tiles, G, tell).span * Hk;
+  int written;
+};
+template <int ROWS, int UG> __device__ __forceinline__ void plan_for(const Kv4Attn &A, int tiles, int G, int lane, bool tell, Plan &p) {
+  const int entries = A.rows.B * tiles;
+  const unsigned Hk = (unsigned)A.c.n_kv_heads;
+  unsigned U = 0;
+  for (int j = 0; j < entries; j += 32) {
+    const Item it = item_of<ROWS, UG>(A, j + lane, tiles, G, tell);
+    const unsigned units = (unsigned)it.span * Hk;
+    U += units;
+    if (entries <= 32) {
+      p.item[lane] = it;
+      p.upto[lane] = scan(units, lane);
+    }
+  }
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) U += __shfl_xor_sync(0xffffffffu, U, o);
-    if (U == 0) return false;
-    const unsigned n = cta_count<ROWS, UG>(U, gridDim.x);
-    if (blockIdx.x >= n) return false;
-    u = units_before(U, blockIdx.x, n);
-    end = units_before(U, blockIdx.x + 1, n);
-    return u < end;
+  for (int o = 16; o > 0; o >>= 1) U += __shfl_xor_sync(0xffffffffu, U, o);
+  const unsigned n = U == 0 ? 0u : cta_count<ROWS, UG>(U, gridDim.x);
+  const bool any = blockIdx.x < n;
+  if (lane < 2) (lane == 0 ? p.u : p.end) = any ? units_before(U, blockIdx.x + lane, n) : 0u;
+  if (lane == 0) p.written = entries <= 32 ? 1 : 0;
+}
+template <int ROWS, int UG> struct Walk {
+  const Plan *plan;
+  unsigned u, end;
+  int tiles;
+  __device__ __forceinline__ void begin(const Plan &p, int n_tiles) {
+    plan = &p;
+    u = p.u;
+    end = p.end;
+    tiles = n_tiles;
   }
   __device__ __forceinline__ bool next(const Kv4Attn &A, int G, int lane, Piece &p) {
     if (u >= end) return false;
     const unsigned Hk = (unsigned)A.c.n_kv_heads;
-    unsigned before = 0;
-    for (int j = 0;; j += 32) {                       // (some item has unit u)
-      const Item it = item_of<ROWS, UG>(A, j + lane, tiles, G, false);
-      const unsigned units = (unsigned)it.span * Hk, upto = before + scan(units, lane);
-      const unsigned hit = __ballot_sync(0xffffffffu, upto > u);
-      if (hit == 0u) {
-        before = __shfl_sync(0xffffffffu, upto, 31);
-        continue;
+    Item it;
+    unsigned upto = 0, before = 0;
+    int e = 0;
+    if (plan->written) {
+      e = __ffs(__ballot_sync(0xffffffffu, plan->upto[lane] > u)) - 1;
+      it = plan->item[e];
+      upto = plan->upto[e];
+    } else {
+      for (int j = 0;; j += 32) {                     // (some item has unit u)
+        const Item mine = item_of<ROWS, UG>(A, j + lane, tiles, G, false);
+        const unsigned sum = before + scan((unsigned)mine.span * Hk, lane);
+        const unsigned hit = __ballot_sync(0xffffffffu, sum > u);
+        if (hit == 0u) {
+          before = __shfl_sync(0xffffffffu, sum, 31);
+          continue;
+        }
+        const int at = __ffs(hit) - 1;
+        e = j + at;
+        it.first = __shfl_sync(0xffffffffu, mine.first, at);
+        it.count = __shfl_sync(0xffffffffu, mine.count, at);
+        it.ctx = __shfl_sync(0xffffffffu, mine.ctx, at);
+        it.kv = __shfl_sync(0xffffffffu, mine.kv, at);
+        it.span = __shfl_sync(0xffffffffu, mine.span, at);
+        upto = __shfl_sync(0xffffffffu, sum, at);
+        break;
       }
-      const int at = __ffs(hit) - 1, e = j + at;
-      p.b = tiles == 1 ? e : e / tiles;
-      p.row0 = (e - p.b * tiles) * ROWS;
-      p.first = __shfl_sync(0xffffffffu, it.first, at);
-      p.count = __shfl_sync(0xffffffffu, it.count, at);
-      p.ctx = __shfl_sync(0xffffffffu, it.ctx, at);
-      p.kv = __shfl_sync(0xffffffffu, it.kv, at);
-      const int span = __shfl_sync(0xffffffffu, it.span, at);
-      const unsigned in = u - __shfl_sync(0xffffffffu, upto - units, at);
-      p.hk = (int)(in / (unsigned)span);
-      const int from = (int)(in - (unsigned)p.hk * (unsigned)span);
-      const int to = (int)min((unsigned)span, (unsigned)from + (end - u));
-      u += (unsigned)(to - from);
-      p.lo = max(0, from - Work<ROWS, UG>::START);
-      p.hi = max(0, to - Work<ROWS, UG>::START);
-      p.begins = from == 0;
-      p.whole = from == 0 && to == span;
-      return true;
     }
+    p.b = tiles == 1 ? e : e / tiles;
+    p.row0 = (e - p.b * tiles) * ROWS;
+    p.first = it.first;
+    p.count = it.count;
+    p.ctx = it.ctx;
+    p.kv = it.kv;
+    const unsigned in = u - (upto - (unsigned)it.span * Hk);
+    p.hk = (int)(in / (unsigned)it.span);
+    const int from = (int)(in - (unsigned)p.hk * (unsigned)it.span);
+    const int to = (int)min((unsigned)it.span, (unsigned)from + (end - u));
+    u += (unsigned)(to - from);
+    p.lo = max(0, from - Work<ROWS, UG>::START);
+    p.hi = max(0, to - Work<ROWS, UG>::START);
+    p.begins = from == 0;
+    p.whole = from == 0 && to == it.span;
+    return true;
   }
 };
 
