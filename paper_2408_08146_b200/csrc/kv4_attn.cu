@@ -24,7 +24,7 @@
 // The softmax is online with a reference maximum that is raised only when a score exceeds it by more than 2^4: in the common
 // case a granule needs no shuffles but one vote.
 // Bound: issue slots.  A granule of 8 rows takes a warp some 300 instructions, half of them to take codes out of words, and four warps on a
-// scheduler issue 0.54 of the time (one sequence of 131071 slots, 8 kv heads: 40.3 us, 3.5 TB/s of the 6.55 that a copy reaches; DRAM 46%, the
+// scheduler issue 0.54 of the time (one sequence of 131071 slots, 8 kv heads: 40.5 us, 3.5 TB/s of the 6.55 that a copy reaches; DRAM 46%, the
 // tensor pipe 22%, the integer pipe 47% of their time).  Tried against it and no faster: codes centred by a second multiply instead of an
 // addition (41.6 us), two granules at a time with tiles of 16 rows, deeper rings.
 #include "kv4_work.cuh"
@@ -79,8 +79,8 @@ __device__ __forceinline__ uint4 lds128(uint32_t at) {
   return v;
 }
 
-// CTAs that share an SM, by registers: as many as there can be (32 ragged sequences up to 8190 slots: 55.3 us with four, 59.1 with three; one of
-// 131071 slots, where three keep their registers: 40.2 and 38.7)
+// CTAs that share an SM, by registers: as many as there can be (32 ragged sequences up to 8190 slots: 44.0 us with four; one of
+// 131071 slots 40.2, with three, which keep their registers, 38.7, but many short items want the fourth)
 template <int NT, bool PAIR> constexpr int CTAS = NT == 1 ? (PAIR ? 3 : 4) : 2;
 template <int NT, bool CLUSTER> constexpr int DEPTH = NT == 1 ? (CLUSTER ? 2 : 3) : 5;      // steps of a warp in its ring
 // Granules per step of a warp: two where registers allow, for independent instructions and half the bookkeeping.

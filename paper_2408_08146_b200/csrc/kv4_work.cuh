@@ -13,10 +13,12 @@
 namespace koala {
 namespace {
 
-// START and the fewest units of a CTA are in units of UG granules
+// START and the fewest units of a CTA are in units of UG granules.  What an item costs to begin, by trial (us; 32 ragged sequences / one of 131071
+// slots with 8, 12, 16, 20, 24 granules: 59.7 / 39.4, 51.8 / 39.3, 47.0 / 40.1, 44.1 / 40.7, 43.8 / 42.3; four 64-row trees with 4, 6, 8, 10, 14
+// tiles: 48.3, 45.6, 45.3, 45.7, 46.3).
 template <int ROWS, int UG> struct Work {
-  static constexpr int START = UG == 1 ? 12 : 6;
-  static constexpr int MIN_UNITS = START + (UG == 1 ? 8 : 2);
+  static constexpr int START = UG == 1 ? 20 : 8;
+  static constexpr int MIN_UNITS = START + (UG == 1 ? 4 : 2);
 };
 
 struct Item {
