@@ -37,9 +37,6 @@ constexpr int INFO = 16;                   // tiles whose parameters are kept (e
 constexpr int BLK = TK * 128;              // [64 keys][64 dims]
 constexpr int ROW_WARPS = 8, EXPANDERS = 8, S_WARP = ROW_WARPS + EXPANDERS, PV_WARP = S_WARP + 1;
 constexpr int THREADS = 32 * (S_WARP + 4);          // whole warpgroups, so that registers can be split
-// Registers a thread: 640 threads start with 96 each, 61440 together; 256 x 128 + 256 x 72 + 128 x 72 = 60416.
-constexpr int REGS_START = 96, REGS_ROWS = 128, REGS_EXPAND = 72, REGS_MMA = 72;
-static_assert(32 * (ROW_WARPS * REGS_ROWS + EXPANDERS * REGS_EXPAND + 4 * REGS_MMA) <= THREADS * REGS_START, "the shares fit in what the block starts with");
 constexpr int E_TIMEOUT = 6;
 constexpr float RAISE = 4.f;
 constexpr int P_TOP = 10;                  // P = 2^P_TOP at the reference maximum
@@ -48,6 +45,15 @@ constexpr int TMEM_COLS = 512;
 
 enum { FULL = 0, HALF = 1, PAIR = 2 };     // 128 rows; 64 rows twice; 64 rows as two values
 template <int MODE> constexpr int TILE_ROWS = MODE == FULL ? 128 : 64;
+// Registers a thread: 640 threads start with 96 each, 61440 together, and that is what is shared out.  The rows get what lets the others do without
+// spilled registers (us, rows / expanding / MMA: 1024 rows of 32 heads with 128 / 72 / 72 172, 128 / 88 / 48 168, 136 / 80 / 48 161, 144 / 80 / 32 162;
+// four 64-row trees with 128 / 72 / 72 44.9, 136 / 80 / 48 43.7, 120 / 88 / 64 43.3).
+constexpr int REGS_START = 96;
+template <int MODE> constexpr int REGS_ROWS = MODE == FULL ? 136 : 120;
+template <int MODE> constexpr int REGS_EXPAND = MODE == FULL ? 80 : 88;
+template <int MODE> constexpr int REGS_MMA = MODE == FULL ? 48 : 64;
+template <int MODE> constexpr bool REGS_FIT = 32 * (ROW_WARPS * REGS_ROWS<MODE> + EXPANDERS * REGS_EXPAND<MODE> + 4 * REGS_MMA<MODE>) <= THREADS * REGS_START;
+static_assert(REGS_FIT<FULL> && REGS_FIT<HALF> && REGS_FIT<PAIR>, "the shares fit in what the block starts with");
 template <int DH> struct Lay {
   static constexpr int ONE = DH / 64 * BLK;
   static constexpr int K = 0, V = NB * ONE, CODES = 2 * NB * ONE;
@@ -202,7 +208,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv4_attn_tc_kernel(const Kv4Attn A
   bool ok = true;
 
   if (warp >= ROW_WARPS && warp < S_WARP) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_EXPAND));
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_EXPAND<MODE>));
     // ------------------------------------------------------------------ expanding warps
     const int w = warp - ROW_WARPS, g = lane >> 2, t = lane & 3;
     const uint32_t codes = sb + LY::CODES + (uint32_t)(w * RING * LY::PART);
@@ -362,7 +368,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv4_attn_tc_kernel(const Kv4Attn A
     }
     if (!ok) atomicExch(&sync.error, 1);
   } else if (warp >= S_WARP) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_MMA));
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_MMA<MODE>));
     // ------------------------------------------------------------------ MMA issuers: one warp for S, one for P V
     // A wait, even for what has long happened, costs the issuer 130 cycles and an MMA 50 to 80: with one warp for both a tile took the
     // 1950 cycles that it spent on two commits, three waits and twelve MMAs in a row.
@@ -408,7 +414,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv4_attn_tc_kernel(const Kv4Attn A
     }
     if (!ok) atomicExch(&sync.error, 1);
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_ROWS));
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_ROWS<MODE>));
     // ------------------------------------------------------------------ rows
     const int quarter = warp & 3, group = warp >> 2;      // tensor-memory lanes 32 quarter ..; tiles with now % 2 == group
     const int half = MODE == FULL ? 0 : lane >> 4;
