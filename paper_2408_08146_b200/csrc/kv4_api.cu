@@ -94,11 +94,11 @@ int koala_kv4_append(const koala_kv4 *k, int32_t layer, const koala_kv4_rows *r,
   if (!cache_ok(k) || !pages_ok(k) || layer < 0 || layer >= k->n_layers || !type_ok(dtype) || !t) return KOALA_E_INVALID;
   const int rc = rows_ok(k, r);
   if (rc != KOALA_OK) return rc;
+  if (r->total == 0) return KOALA_OK;
   const bool queries = t[2].data != nullptr;
   if (!tensor_ok(t[0], dtype) || !tensor_ok(t[1], dtype)) return KOALA_E_INVALID;
   if (queries && (!tensor_ok(t[2], dtype) || !tensor_ok(t[3], dtype) || n_heads < 1 || n_heads > 65536)) return KOALA_E_INVALID;
   if (rope && (n_pos < 1 || ((uintptr_t)rope & 15u) != 0)) return KOALA_E_INVALID;
-  if (r->total == 0) return KOALA_OK;
   const Kv4Tensor x[3] = {queries ? tensor_of(t[2]) : Kv4Tensor{nullptr, 0, 0}, tensor_of(t[0]), tensor_of(t[1])};
   return done(kv4_append(Launch{(cudaStream_t)cuda_stream, true}, k->head_dim, dtype, cache_of(k, r->page_table, r->table_stride),
                          (size_t)layer * layer_bytes(k), rows_of(r), x, queries ? n_heads : 0, queries ? tensor_of(t[3]) : Kv4Tensor{nullptr, 0, 0}, rope,
@@ -115,10 +115,10 @@ int koala_kv4_attention(const koala_kv4 *k, int32_t layer, const koala_kv4_rows 
   if (!cache_ok(k) || !pages_ok(k) || layer < 0 || layer >= k->n_layers || !type_ok(dtype) || !t) return KOALA_E_INVALID;
   const int rc = rows_ok(k, r);
   if (rc != KOALA_OK) return rc;
-  if (!tensor_ok(t[0], dtype) || !tensor_ok(t[1], dtype)) return KOALA_E_INVALID;
   if (n_heads < 1 || n_heads > 65536 || n_heads % k->n_kv_heads != 0 || !(scale > 0.f && scale < 1e30f)) return KOALA_E_INVALID;
   if (too_much(k, r, n_heads)) return KOALA_E_UNSUPPORTED;
   if (r->total == 0) return KOALA_OK;
+  if (!tensor_ok(t[0], dtype) || !tensor_ok(t[1], dtype)) return KOALA_E_INVALID;
   if (!scratch || scratch_bytes < koala_kv4_attention_scratch_bytes(k, r, n_heads)) return KOALA_E_CAPACITY;
   if (((uintptr_t)scratch & 15u) != 0) return KOALA_E_INVALID;
   const Kv4Attn a{cache_of(k, r->page_table, r->table_stride), (size_t)layer * layer_bytes(k), rows_of(r), tensor_of(t[0]), tensor_of(t[1]), nullptr,
@@ -142,7 +142,7 @@ int koala_kv4_read(const koala_kv4 *k, int32_t layer, const koala_kv4_rows *r, i
 
 int koala_kv4_move(const koala_kv4 *k, int32_t B, const int32_t *page_table, int32_t table_stride, int32_t n, const int32_t *src, const int32_t *dst,
                    int32_t *status, void *cuda_stream) {
-  if (!cache_ok(k) || !pages_ok(k) || B < 1 || B > 65535 || !page_table || table_stride < 1 || n < 0 || !src || !dst) return KOALA_E_INVALID;
+  if (!cache_ok(k) || !pages_ok(k) || B < 1 || B > 65535 || !page_table || table_stride < 1 || n < 0 || (n > 0 && (!src || !dst))) return KOALA_E_INVALID;
   if ((long long)table_stride * k->page_size > (1ll << 30)) return KOALA_E_INVALID;
   if (n > KV4_MAX_MOVES || (long long)k->n_layers * k->n_kv_heads > (1 << 30)) return KOALA_E_UNSUPPORTED;
   if (n == 0) return KOALA_OK;

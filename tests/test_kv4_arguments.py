@@ -107,6 +107,18 @@ def test_scratch_of_the_attention():
     assert lib.koala_kv4_attention(C.byref(cache_c()), 0, C.byref(rows_c(max_rows=1 << 20, total=1, row_start=4096)), 1, tensors(GOOD, GOOD), 4, 0.1, 4096, 1 << 40, None) == UNSUPPORTED
 
 
+def test_no_rows_need_no_tensors():
+    """A step without rows passes, whatever an empty tensor's address is; what else is wrong is still refused."""
+    none, empty = (0, 512, 128), rows_c(total=0, row_start=4096)
+    assert append(cache_c(), empty, t=(none, none, none, none)) == 0
+    assert attention(cache_c(), empty, t=(none, none)) == 0
+    assert m._library().koala_kv4_read(C.byref(cache_c()), 0, C.byref(empty), 1, tensors(none, none), None, None) == 0
+    move = lambda n, at: m._library().koala_kv4_move(C.byref(cache_c()), 2, 4096, 4, n, at, at, None, None)
+    assert move(0, None) == 0 and move(1, None) == INVALID
+    assert append(cache_c(), empty, t=(none,) * 4, layer=2) == INVALID
+    assert attention(cache_c(), empty, t=(none, none), heads=3) == INVALID
+
+
 def test_more_work_than_is_counted():
     """Units of work are counted in 32 bits."""
     for c, r in ((cache_c(n_kv_heads=1), rows_c(B=60000, total=60000, table_stride=1 << 26)),
