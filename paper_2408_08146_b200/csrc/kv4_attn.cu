@@ -599,11 +599,11 @@ template <int DH, int NT, bool PAIR> cudaError_t go(Launch L, const Kv4Attn &a, 
 
 // CTAs of a cluster that takes an item, 0: the items are to be dealt evenly instead.  The host knows how many slots a page-table row names, not
 // how many are in use, so the rule goes by these.  A cluster has no second launch and no plan to work out: us by slots, clusters / dealt,
-//   1 row of 32 heads      192: 6.6 / 13.1   1024: 7.5 / 13.8   4096: 11.3 / 16.9   8192: 16.6 / 19.6   16384: 26.9 / 26.7
-//   the same, batch 32     192: 18 / 30      577: 28 / 42       1024: 39 / 55       2048: 65 / 80
-//   60 rows of 32 heads    192: 11.4 / 23.7  1024: 15.7 / 22.3  2048: 21.5 / 24.8   4096: 33.4 / 29.2
-//   the same, fp32         192: 12.5 / 24.9  1024: 19.6 / 23.6  2048: 28.8 / 25.9
-// (beyond 16 rows "dealt" is kv4_attn_tc.cu).  So up to 16 granules a warp, 32 where the items fill the machine and there is nothing to deal, 12 where a
+//   1 row of 32 heads      192: 6.6 / 12.0   1024: 7.6 / 12.2   4096: 11.4 / 15.6  8192: 16.5 / 18.3  16384: 26.9 / 26.7
+//   the same, batch 32     192: 18 / 28      577: 27 / 40       1024: 39 / 53      2048: 64 / 78
+//   60 rows of 32 heads    192: 11.5 / 17.5  1024: 15.6 / 21.3  2048: 21.4 / 21.1
+//   the same, fp32         192: 12.7 / 18.1  1024: 19.6 / 22.6  1536: 24.2 / 22.7
+// (beyond 16 rows "dealt" is kv4_attn_tc.cu).  So up to 16 granules a warp, 32 where the items fill the machine and there is nothing to deal, 10 where a
 // granule is twice the work; with tiles of 16 rows only what is resident at once, in clusters of four (of eight not all are placed at once:
 // 16 rows of 32 heads at 577 slots 14.0 us, of four 10.0).
 template <int NT, bool PAIR> int cluster_of(const Kv4Attn &a, int num_sms) {
@@ -613,7 +613,7 @@ template <int NT, bool PAIR> int cluster_of(const Kv4Attn &a, int num_sms) {
   if (tile_rows > 65535 || a.c.n_kv_heads > 65535 || (NT == 2 && items > resident)) return 0;
   int n = NT == 1 ? PEERS : PEERS / 2;
   while (n > 1 && (items * n > resident || granules <= n / 2 * WARPS * STEP<NT>)) n /= 2;
-  const int most = NT == 1 ? (2 * items * n > resident ? 32 : 16) : PAIR ? 12 : 16;
+  const int most = NT == 1 ? (2 * items * n > resident ? 32 : 16) : PAIR ? 10 : 16;
   return granules <= (long long)n * WARPS * most ? n : 0;
 }
 template <int DH, int NT, bool PAIR> cudaError_t go_cluster(Launch L, const Kv4Attn &a, int peers) {
